@@ -302,11 +302,11 @@ def _values(st, pages, kv):
 
 
 def _power(amax, log2_top, mantissa_top):
-    """The smallest power of two s with top * s >= amax; 1 where amax is 0.
+    """The smallest power of two s >= 2^-126 with top * s >= amax, where
     top = 2 * mantissa_top * 2^log2_top."""
     m, e = torch.frexp(amax)
-    e = (e - 1 - log2_top + (m > mantissa_top)).clamp(-126, 120)
-    return torch.where(amax > 0, ((e + 127).int() << 23).view(torch.float32), 1.0)
+    e = torch.where(amax > 0, e - 1 - log2_top + (m > mantissa_top), -126).clamp(-126, 127)
+    return ((e + 127).int() << 23).view(torch.float32)
 
 
 def _bounds_of(keys, there):
