@@ -542,6 +542,162 @@ int ea_layer_checksum(ea_cache *cache, int32_t layer, const int32_t *pages,
                       int32_t n, uint64_t *d_out, int64_t out_capacity,
                       hipStream_t stream);
 
+/* ------------------------------------------------------- cache operators
+ *
+ * What a serving step does with one layer of the paged cache (not in the
+ * paper, whose serving engine does it): append new tokens, attend to the
+ * cached ones, select the blocks worth attending to.
+ *
+ * Cache: elem_bytes 2 holds activations' own type (dtype below), elem_bytes
+ * 1 holds fp8 e4m3 (largest value 448) with scales: a stored value is its
+ * code times its scale.  head_dim must be a multiple of 8 and at most 256,
+ * num_pages * page_tokens below 2^31 (EA_ENOTSUP otherwise); page_tokens may
+ * be any, and multiples of 16 are fastest.
+ *
+ * Everything a call reads or writes is device memory, page tables, lengths
+ * and selections too, so a step crosses no host link and can be captured in a
+ * graph; the calls allocate nothing and are asynchronous on `stream`.  The
+ * host cannot see device values, so the kernels hold them to the bounds given:
+ * a page id outside [0, num_pages) holds no tokens, a kv_len is taken as at
+ * most max_kv and at least 0, row_start as inside [0, n_rows], rows of a
+ * sequence beyond max_rows are left unwritten. */
+
+typedef enum { EA_BF16 = 0, EA_F16 = 1 } ea_dtype;
+
+/* Per-block planes beside the cache, each optional (NULL):
+ *  head_scales   float32 [L][P][2][H]: a scale for each block and head (K, V).
+ *                Without it an fp8 cache takes its scale plane [L][P][2], one
+ *                scale for all heads of a block; appending then needs H = 1.
+ *  bounds        int8 [L][P][2][H][D]: lowest (rounded down) and highest
+ *                (rounded up) key element of a block, in units of
+ *  bound_scales  float32 [L][P][H], powers of two.
+ * A plane is itself an ea_cache of page_tokens 1 (head_scales: head_dim 1,
+ * elem_bytes 4; bounds: elem_bytes 1) where its pieces are whole 16 bytes, so
+ * it can go to a tier of its own beside the cache's blocks; bounds can also be
+ * made again from restored blocks (ea_bound_blocks). */
+typedef struct {
+  float *head_scales;
+  int8_t *bounds;      /* 8-byte aligned */
+  float *bound_scales;
+} ea_cache_planes;
+
+/* The sequences of a step.  Sequence s owns rows row_start[s] ..
+ * row_start[s+1]-1 of the step's tokens (row_start NULL: row s), which are the
+ * last of its kv_len[s] tokens; token i lies in slot i mod T of page
+ * page_table[s*table_stride + i/T]. */
+typedef struct {
+  const int32_t *page_table; /* int32[n_seqs][table_stride]                   */
+  const int32_t *kv_len;     /* int32[n_seqs]: tokens with this step's        */
+  const int32_t *row_start;  /* int32[n_seqs+1] non-decreasing, or NULL       */
+  int64_t table_stride;      /* * page_tokens >= max_kv                       */
+  int32_t n_seqs;
+  int32_t n_rows;            /* rows of all sequences                         */
+  int32_t max_rows;          /* most rows of one sequence                     */
+  int32_t max_kv;            /* most kv_len; at most 2^30                     */
+} ea_batch;
+
+/* Rows of heads of dtype elements: element (row, head, d) at
+ * data[row*row_stride + head*head_stride + d].  data 16-byte aligned, strides
+ * multiples of 8 elements (slices of a fused projection's rows fit). */
+typedef struct {
+  void *data;
+  int64_t row_stride;
+  int64_t head_stride;
+} ea_rows;
+
+typedef struct {
+  ea_rows k, v;        /* [n_rows][H][D]                                      */
+  ea_rows q, q_out;    /* [n_rows][q_heads][D]; q.data NULL: no queries.
+                          q_out may be q                                      */
+  const float *rope;   /* float32 [rope_len][rope_dim], 16-byte aligned: the
+                          cosines of a position, then its sines (rope_dim / 2
+                          each); NULL: keys and queries stay as they are      */
+  int32_t rope_len;    /* >= max_kv                                           */
+  int32_t rope_dim;    /* even, <= head_dim: the leading elements that turn   */
+  int32_t interleaved; /* pairs (2i, 2i+1) instead of (i, i + rope_dim/2)     */
+  int32_t q_heads;
+  int32_t dtype;       /* ea_dtype of k, v, q, q_out                          */
+  int32_t _pad;
+} ea_append;
+
+/* Append a step's tokens to layer `layer`: row r of sequence s goes to
+ * position kv_len[s] - rows + r, its key rotated by the position's angles in
+ * 32 bits and rounded once, its value as it is; q_out gets the rotated
+ * queries.  In an fp8 cache a block and head's scale is the smallest power of
+ * two that holds the block's largest finite magnitude; a block that held
+ * older tokens keeps its scale unless the new tokens need a larger one, and
+ * then the older codes are requantised to it.  Values that are not finite
+ * become NaN.  With bounds, the touched blocks' bounds are made from all
+ * their stored keys.  Pages that get new tokens must belong to one sequence
+ * of the batch alone; a prefix shared by several is fine. */
+int ea_append_kv(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,
+                 const ea_batch *batch, const ea_append *args, hipStream_t stream);
+
+/* Bounds of whole blocks from their stored keys (blocks restored from a
+ * tier, written by another engine): pages d_pages[0..n) (device int32; ids
+ * outside the cache are skipped) of layers [layer_begin, layer_begin +
+ * layer_count).  dtype: of a 16-bit cache. */
+int ea_bound_blocks(ea_cache *cache, const ea_cache_planes *planes, int32_t layer_begin,
+                    int32_t layer_count, const int32_t *d_pages, int32_t n, int32_t dtype,
+                    hipStream_t stream);
+
+typedef struct {
+  ea_rows q, out;          /* [n_rows][q_heads][D]                            */
+  float *lse;              /* float32 [n_rows][q_heads] or NULL: natural log of
+                              the sum of exponentials, -inf for an empty row  */
+  const int32_t *selected; /* int32 [n_rows][H][budget] or NULL: the blocks
+                              (positions in the page table) a row's KV head
+                              attends to; others, as -1, are skipped          */
+  int32_t budget;
+  int32_t window;          /* > 0: only the last `window` tokens up to a row's
+                              own; 0: all.  Must be 0 with `selected`         */
+  int32_t q_heads;         /* a multiple of the cache's H                     */
+  int32_t dtype;           /* ea_dtype of q and out                           */
+  float scale;             /* softmax scale, > 0 and finite                   */
+  int32_t _pad;
+} ea_attention;
+
+/* Attention of a step's queries over layer `layer`: row r of sequence s, at
+ * position p = kv_len[s] - rows + r, attends to the tokens j <= p of its
+ * sequence (j > p - window; in its selected blocks), query head i to KV head
+ * i / (q_heads / H).  Sums and softmax statistics are 32 bits.  A row that
+ * attends to nothing gets zeros.  What lies in slots that no row of the
+ * sequence attends to never matters.  workspace (16-byte aligned device
+ * memory, ea_attend_workspace bytes; NULL when that is 0) is scratch of this
+ * call: calls that may overlap need their own. */
+int64_t ea_attend_workspace(const ea_cache *cache, const ea_batch *batch,
+                            const ea_attention *args);
+int ea_attend(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,
+              const ea_batch *batch, const ea_attention *args, void *workspace,
+              int64_t workspace_bytes, hipStream_t stream);
+
+typedef struct {
+  ea_rows q;          /* [n_rows][q_heads][D], rotated as the keys are        */
+  int32_t *selected;  /* int32 [n_rows][H][budget]                            */
+  int32_t budget;     /* blocks of a row and KV head                          */
+  int32_t first;      /* the first blocks and                                 */
+  int32_t last;       /* the row's last ones (its own among them) are always
+                         taken: first, last >= 0, first + last <= budget      */
+  int32_t q_heads;
+  int32_t dtype;      /* ea_dtype of q                                        */
+  int32_t _pad;
+} ea_selection;
+
+/* Blocks for sparse attention from the bounds planes.  A block's score for a
+ * row and KV head is the largest over the group's query heads of
+ *   sum_d max(c_d lo_d, c_d hi_d) * unit(q) * bound_scale,
+ * c = q rounded to whole numbers within 127 in units of the smallest power of
+ * two that allows it: an upper bound of the score of any key of the block, up
+ * to the rounding of q, exact in 32 bits.  The `budget` highest blocks at or
+ * before the row's own are listed in increasing order, ties going to the
+ * lower block; fewer blocks leave -1 at the end.  At most 65,536 blocks a
+ * sequence (EA_ENOTSUP). */
+int64_t ea_select_workspace(const ea_cache *cache, const ea_batch *batch,
+                            const ea_selection *args);
+int ea_select_blocks(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,
+                     const ea_batch *batch, const ea_selection *args, void *workspace,
+                     int64_t workspace_bytes, hipStream_t stream);
+
 /* How stores and loads cross the host link:
  *  EA_PLAN_DIRECT: one kernel reads/writes the mapped pinned slots;
  *  EA_PLAN_STAGED: gather/scatter through an HBM staging buffer plus DMA

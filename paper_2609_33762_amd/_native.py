@@ -18,6 +18,7 @@ EA_ADMIT_CONDITIONED, EA_ADMIT_ALWAYS, EA_ADMIT_FIXED = 0, 1, 2
 EA_PLAN_AUTO, EA_PLAN_DIRECT, EA_PLAN_STAGED = 0, 1, 2
 EA_DIR_STORE, EA_DIR_LOAD, EA_DIR_BOTH = 0, 1, 2
 EA_SLOT_FREE, EA_SLOT_PENDING, EA_SLOT_RESIDENT = 0, 1, 2
+EA_BF16, EA_F16 = 0, 1
 
 
 class CacheDesc(C.Structure):
@@ -70,6 +71,39 @@ class ControllerConfig(C.Structure):
                 ("manual_clock", C.c_int32), ("_pad", C.c_int32)]
 
 
+class CachePlanes(C.Structure):
+    _fields_ = [("head_scales", C.c_void_p), ("bounds", C.c_void_p),
+                ("bound_scales", C.c_void_p)]
+
+
+class BatchDesc(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("row_start", C.c_void_p),
+                ("table_stride", C.c_int64), ("n_seqs", C.c_int32), ("n_rows", C.c_int32),
+                ("max_rows", C.c_int32), ("max_kv", C.c_int32)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Append(C.Structure):
+    _fields_ = [("k", Rows), ("v", Rows), ("q", Rows), ("q_out", Rows), ("rope", C.c_void_p),
+                ("rope_len", C.c_int32), ("rope_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("q_heads", C.c_int32), ("dtype", C.c_int32), ("_pad", C.c_int32)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("q", Rows), ("out", Rows), ("lse", C.c_void_p), ("selected", C.c_void_p),
+                ("budget", C.c_int32), ("window", C.c_int32), ("q_heads", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("_pad", C.c_int32)]
+
+
+class Selection(C.Structure):
+    _fields_ = [("q", Rows), ("selected", C.c_void_p), ("budget", C.c_int32),
+                ("first", C.c_int32), ("last", C.c_int32), ("q_heads", C.c_int32),
+                ("dtype", C.c_int32), ("_pad", C.c_int32)]
+
+
 class ControllerStatus(C.Structure):
     _fields_ = [("now", C.c_int64), ("reports_published", C.c_int64),
                 ("published", TierReport), ("seen", TierReport),
@@ -113,6 +147,12 @@ SIGNATURES = {
     "ea_gather_blocks": (_INT, [_P, _P, _I32, _P, _I64, _P]),
     "ea_scatter_blocks": (_INT, [_P, _P, _I64, _P, _I32, _P]),
     "ea_layer_checksum": (_INT, [_P, _I32, _P, _I32, _P, _I64, _P]),
+    "ea_append_kv": (_INT, [_P, _P, _I32, _P, _P, _P]),
+    "ea_bound_blocks": (_INT, [_P, _P, _I32, _I32, _P, _I32, _I32, _P]),
+    "ea_attend_workspace": (_I64, [_P, _P, _P]),
+    "ea_attend": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
+    "ea_select_workspace": (_I64, [_P, _P, _P]),
+    "ea_select_blocks": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
     "ea_tier_set_plan": (_INT, [_P, _INT, _INT]),
     "ea_tier_get_plan": (_INT, [_P, _INT, _P]),
     "ea_peak_probe": (_INT, [_P, _P, _I64, _INT, _INT, _P]),

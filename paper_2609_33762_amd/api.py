@@ -57,10 +57,15 @@ def _stream(s):
 class Cache:
     """A caller-owned paged KV cache: `kv` is a CUDA tensor holding
     [L][P][2][T][H][D] elements of elem_bytes each (any dtype, contiguous);
-    `scales` an optional contiguous CUDA float32 tensor [L][P][2]."""
+    `scales` an optional contiguous CUDA float32 tensor [L][P][2].
+
+    The planes of the cache operators are optional contiguous CUDA tensors
+    beside it: `head_scales` float32 [L][P][2][H], `bounds` int8
+    [L][P][2][H][D] and `bound_scales` float32 [L][P][H]."""
 
     def __init__(self, kv, num_pages, num_layers, page_tokens, num_kv_heads,
-                 head_dim, elem_bytes, scales=None):
+                 head_dim, elem_bytes, scales=None, head_scales=None, bounds=None,
+                 bound_scales=None):
         lib = N.load()
         assert kv.is_cuda and kv.is_contiguous()
         piece = 2 * page_tokens * num_kv_heads * head_dim * elem_bytes
@@ -81,6 +86,21 @@ class Cache:
         self.slot_bytes = num_layers * piece + trailer
         self._h = C.c_void_p()
         N.check("ea_cache_create", lib.ea_cache_create(C.byref(self.desc), C.byref(self._h)))
+        self.num_kv_heads, self.head_dim, self.elem_bytes = num_kv_heads, head_dim, elem_bytes
+        self.page_tokens = page_tokens
+        blocks = num_layers * num_pages * num_kv_heads
+        for name, t, dtype, need in (("head_scales", head_scales, "torch.float32", 2 * blocks),
+                                     ("bounds", bounds, "torch.int8", 2 * blocks * head_dim),
+                                     ("bound_scales", bound_scales, "torch.float32", blocks)):
+            if t is None:
+                continue
+            if not t.is_cuda or not t.is_contiguous() or str(t.dtype) != dtype:
+                raise ValueError(f"{name} must be a contiguous {dtype} device tensor")
+            if t.numel() < need:
+                raise ValueError(f"{name} holds {t.numel()} values, the cache needs {need}")
+        self.head_scales, self.bounds, self.bound_scales = head_scales, bounds, bound_scales
+        self._planes = N.CachePlanes(*(None if t is None else t.data_ptr()
+                                       for t in (head_scales, bounds, bound_scales)))
 
     @property
     def handle(self):
@@ -126,6 +146,178 @@ class Cache:
             raise ValueError("d_out must be a contiguous 64-bit device tensor of len(pages)")
         N.check("ea_layer_checksum", N.load().ea_layer_checksum(
             self._h, layer, _ptr(p), len(p), d_out.data_ptr(), d_out.numel(), _stream(stream)))
+
+
+    # ------------------------------------------------------ cache operators
+    def _fits(self, batch):
+        if batch.max_kv > batch.pages * self.page_tokens:
+            raise ValueError(f"page_table holds {batch.pages} pages of {self.page_tokens} tokens "
+                             f"a sequence, max_kv is {batch.max_kv}")
+
+    def append_kv(self, layer, batch, k, v, rope=None, q=None, q_out=None, interleaved=False,
+                  stream=None):
+        """Append a step's tokens: k, v [n_rows, H, D] (any row and head
+        strides) go to the last positions of their sequences, keys rotated
+        by `rope` (float32 [positions, rope_dim], cosines then sines); q_out
+        gets q rotated (it may be q)."""
+        self._fits(batch)
+        act = _dtype(k)
+        if _dtype(v) != act:
+            raise ValueError("k and v must have one dtype")
+        a = N.Append(k=_rows(k, "k", batch.n_rows, self.num_kv_heads, self.head_dim),
+                     v=_rows(v, "v", batch.n_rows, self.num_kv_heads, self.head_dim),
+                     interleaved=int(interleaved), dtype=act)
+        if q is not None:
+            if q_out is None or _dtype(q) != act or _dtype(q_out) != act:
+                raise ValueError("q needs a q_out, both of k's dtype")
+            a.q = _rows(q, "q", batch.n_rows, q.shape[1], self.head_dim)
+            a.q_out = _rows(q_out, "q_out", batch.n_rows, q.shape[1], self.head_dim)
+            a.q_heads = q.shape[1]
+        if rope is not None:
+            if not rope.is_cuda or str(rope.dtype) != "torch.float32" or rope.dim() != 2 or \
+                    not rope.is_contiguous():
+                raise ValueError("rope must be a contiguous float32 device matrix")
+            a.rope, a.rope_len, a.rope_dim = rope.data_ptr(), rope.shape[0], rope.shape[1]
+        N.check("ea_append_kv", N.load().ea_append_kv(
+            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
+            _stream(stream)))
+
+    def bound_blocks(self, d_pages, layer_begin=0, layer_count=None, dtype=None, stream=None):
+        """Bounds of whole blocks from their stored keys; d_pages: int32
+        device tensor.  dtype: of a 16-bit cache (torch.bfloat16 if None)."""
+        _device_ints(d_pages, "d_pages")
+        count = self.num_layers - layer_begin if layer_count is None else layer_count
+        act = N.EA_BF16 if dtype is None else _ACT[str(dtype)]
+        N.check("ea_bound_blocks", N.load().ea_bound_blocks(
+            self._h, C.byref(self._planes), layer_begin, count, d_pages.data_ptr(),
+            d_pages.numel(), act, _stream(stream)))
+
+    def attend(self, layer, batch, q, out, scale=None, window=0, selected=None, lse=None,
+               stream=None):
+        """Attention of q [n_rows, q_heads, D] over the cached tokens up to
+        each row's own, into out; scale: 1/sqrt(D) if None; window > 0: the
+        last tokens only; selected int32 [n_rows, H, budget]: those blocks
+        only (see select_blocks); lse: float32 [n_rows, q_heads] output."""
+        self._fits(batch)
+        if _dtype(q) != _dtype(out):
+            raise ValueError("q and out must have one dtype")
+        a = N.Attention(q=_rows(q, "q", batch.n_rows, q.shape[1], self.head_dim),
+                        out=_rows(out, "out", batch.n_rows, q.shape[1], self.head_dim),
+                        window=window, q_heads=q.shape[1], dtype=_dtype(q),
+                        scale=self.head_dim ** -0.5 if scale is None else scale)
+        if selected is not None:
+            _selection(selected, batch.n_rows, self.num_kv_heads)
+            a.selected, a.budget = selected.data_ptr(), selected.shape[2]
+        if lse is not None:
+            if not lse.is_cuda or str(lse.dtype) != "torch.float32" or \
+                    not lse.is_contiguous() or tuple(lse.shape) != (batch.n_rows, q.shape[1]):
+                raise ValueError("lse must be a contiguous float32 device tensor "
+                                 "[n_rows, q_heads]")
+            a.lse = lse.data_ptr()
+        lib, s = N.load(), _stream(stream)
+        need = lib.ea_attend_workspace(self._h, C.byref(batch.desc), C.byref(a))
+        if need < 0:
+            N.check("ea_attend_workspace", need)
+        N.check("ea_attend", lib.ea_attend(
+            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
+            batch.workspace(need, s), need, s))
+
+    def select_blocks(self, layer, batch, q, selected, first=1, last=1, stream=None):
+        """Blocks for sparse attention of q's rows from the bounds planes:
+        selected int32 [n_rows, H, budget] gets the positions (in the page
+        table) of the highest-scored blocks in increasing order, the `first`
+        blocks and the row's `last` ones always among them, -1 at the end."""
+        self._fits(batch)
+        _selection(selected, batch.n_rows, self.num_kv_heads)
+        a = N.Selection(q=_rows(q, "q", batch.n_rows, q.shape[1], self.head_dim),
+                        selected=selected.data_ptr(), budget=selected.shape[2], first=first,
+                        last=last, q_heads=q.shape[1], dtype=_dtype(q))
+        lib, s = N.load(), _stream(stream)
+        need = lib.ea_select_workspace(self._h, C.byref(batch.desc), C.byref(a))
+        if need < 0:
+            N.check("ea_select_workspace", need)
+        N.check("ea_select_blocks", lib.ea_select_blocks(
+            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
+            batch.workspace(need, s), need, s))
+
+
+_ACT = {"torch.bfloat16": N.EA_BF16, "torch.float16": N.EA_F16}
+
+
+def _dtype(t):
+    act = _ACT.get(str(t.dtype))
+    if act is None:
+        raise ValueError(f"rows must be bfloat16 or float16, not {t.dtype}")
+    return act
+
+
+def _rows(t, what, n_rows, heads, head_dim):
+    if not t.is_cuda or t.dim() != 3 or t.shape[0] < n_rows or \
+            tuple(t.shape[1:]) != (heads, head_dim) or t.stride(2) != 1:
+        raise ValueError(f"{what} must be a device tensor [{n_rows}, {heads}, {head_dim}] "
+                         "whose last dimension is contiguous")
+    return N.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _device_ints(t, what):
+    if not t.is_cuda or str(t.dtype) != "torch.int32" or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 device tensor")
+
+
+def _selection(t, n_rows, heads):
+    _device_ints(t, "selected")
+    if t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != heads:
+        raise ValueError(f"selected must be [{n_rows}, {heads}, budget]")
+
+
+class Batch:
+    """The sequences of a serving step, on the device: `page_table` int32
+    [n_seqs, pages], `kv_len` int32 [n_seqs] (tokens with the step's own),
+    `row_start` int32 [n_seqs + 1] or None (one row each).  max_kv and
+    max_rows bound what the device values hold.  Keeps the scratch of the
+    calls made with it, one buffer for each stream."""
+
+    def __init__(self, page_table, kv_len, max_kv, row_start=None, n_rows=None, max_rows=None):
+        if not page_table.is_cuda or str(page_table.dtype) != "torch.int32" or \
+                page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be an int32 device matrix with contiguous rows")
+        _device_ints(kv_len, "kv_len")
+        n = page_table.shape[0]
+        if kv_len.numel() != n:
+            raise ValueError("kv_len needs one length for each row of page_table")
+        if row_start is None:
+            n_rows, max_rows = n, min(n, 1)
+        else:
+            _device_ints(row_start, "row_start")
+            if row_start.numel() != n + 1:
+                raise ValueError("row_start needs one entry more than page_table has rows")
+            if n_rows is None or max_rows is None:
+                raise ValueError("row_start needs n_rows and max_rows")
+        self.page_table, self.kv_len, self.row_start = page_table, kv_len, row_start
+        self.n_rows, self.max_rows, self.max_kv = n_rows, max_rows, max_kv
+        self.pages = page_table.shape[1]  # of a row; rows may lie further apart
+        self.desc = N.BatchDesc(page_table.data_ptr(), kv_len.data_ptr(),
+                                None if row_start is None else row_start.data_ptr(),
+                                page_table.stride(0) if n > 1 else self.pages, n, n_rows,
+                                max_rows, max_kv)
+        self._scratch = {}
+
+    def workspace(self, nbytes, stream):
+        """Device scratch of at least nbytes for calls on this stream."""
+        import torch
+        if nbytes == 0:
+            return None
+        t = self._scratch.get(stream)
+        if t is None or t.numel() < nbytes:
+            # taken on the calls' own stream: the allocator orders reuse by it
+            if stream == current_stream():
+                t = torch.empty(nbytes, dtype=torch.uint8, device=self.kv_len.device)
+            else:
+                s = torch.cuda.ExternalStream(stream, device=self.kv_len.device)
+                with torch.cuda.stream(s):
+                    t = torch.empty(nbytes, dtype=torch.uint8, device=self.kv_len.device)
+            self._scratch[stream] = t
+        return t.data_ptr()
 
 
 def make_policy(kappa, block_tokens, beta_rank, theta_ppm=950000, activity_window=64,

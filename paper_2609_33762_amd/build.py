@@ -18,7 +18,9 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libea.so")
 SOURCES = ["ea_copy_kernels.hip", "ea_sha256_kernels.hip", "ea_tier_meta.cpp",
-           "ea_api.cpp", "ea_hash.cpp", "ea_stack.cpp", "ea_controller.cpp"]
+           "ea_api.cpp", "ea_hash.cpp", "ea_stack.cpp", "ea_controller.cpp",
+           "ea_attend_split.hip", "ea_attend_chunk.hip", "ea_select_kernels.hip",
+           "ea_append_kernels.hip", "ea_kv_ops.cpp"]
 ARCH = "gfx950"
 
 

@@ -370,6 +370,11 @@ struct ea_cache {
   IndexRing ring;
 };
 
+namespace ea {
+const ea_cache_desc &cache_desc(const ea_cache *c) { return c->d; }
+int cache_device(const ea_cache *c) { return c->device; }
+}  // namespace ea
+
 // ------------------------------------------------------------------- tier
 
 namespace {

@@ -1,0 +1,352 @@
+// Attention of many query rows over the paged cache: chunks of a prompt.
+//
+// The mathematics is the split kernel's; here the matrix products bound it.
+// A workgroup of four waves takes 128 rows (query rows times the heads of a
+// KV head's group, so a key is loaded once for all of them) and walks the
+// tokens in tiles of 64 that its waves share through LDS; a wave keeps 32
+// rows.  The products are transposed (S^T = K Q^T, O^T = V^T P^T): a lane
+// holds scores of one row only, so the softmax is its own work but for one
+// exchange with the lane 32 away, and P goes from the scores' registers into
+// the second product as it is.  V^T comes from LDS through transposing reads.
+//
+// fp8 keys and values become 16-bit values, exactly, on their way into LDS.
+// A key's scale multiplies its scores.  A value's scale, relative to the
+// largest one so far, multiplies its weight: both stay 32 bits until the
+// weight is rounded to f16, whose range the relative scale and the running
+// maximum hold.
+#include <hip/hip_runtime.h>
+
+#include "ea_kv_device.hpp"
+
+namespace ea {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kLanes;
+constexpr int kTok = kChunkTokens;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <int ACT, bool FP8, int DT>
+__global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(AttendArgs a) {
+  constexpr int DP = DT * 32;
+  constexpr int CH = DP / 8;                  // chunks of 8 elements of a head
+  constexpr int PASS = kTok * CH / kThreads;  // chunks a thread stages
+  constexpr int STEP = kThreads / CH;         // tokens of a pass
+  constexpr int PV = FP8 ? kF16 : ACT;
+  constexpr float kShift = PV == kF16 ? 15.f : 0.f;
+  constexpr int EB = FP8 ? 1 : 2;
+  // pitches: eight tokens' 16 bytes of keys, and four tokens' 32 bytes of
+  // values, fall on different banks
+  constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32;
+  __shared__ __align__(16) uint8_t k_lds[kTok * KP];
+  __shared__ __align__(16) uint8_t v_lds[kTok * VP];
+  __shared__ __align__(16) float ks_lds[kTok], vs_lds[kTok];
+
+  const KvLayer &kv = a.kv;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, gg = lane >> 5;
+  const int wave = uniform(tid >> 6);
+  const int H = kv.heads, D = kv.head_dim, T = kv.page_tokens, G = a.group;
+  const int tiles_most = (a.b.max_rows * G + kChunkRows - 1) / kChunkRows;
+
+  uint32_t u = blockIdx.x;
+  const int h = u % H;
+  u /= H;
+  const int part = u % a.splits;
+  u /= a.splits;
+  const int tile = tiles_most - 1 - u % tiles_most;  // longest first
+  const int s = u / tiles_most;
+  const Seq sq = sequence(a.b, s);
+  if (sq.rows * G <= a.split_rows_most || tile * kChunkRows >= sq.rows * G) return;
+  const int pos0 = sq.len - sq.rows;
+  const Span span = span_of(a, sq, pos0);
+  if (part >= span.parts) return;
+  const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
+  const int last_page = sq.len > 0 ? over_page(kv, sq.len - 1) : 0;
+
+  // rows: r of the sequence is query row r / G, head r % G of the group
+  const int r = tile * kChunkRows + wave * 32 + c, qi = r / G;
+  const bool there = qi < sq.rows;
+  const int lim = there ? min(pos0 + qi + 1, sq.len) : 0;
+  const int low = there && a.window > 0 ? max(0, pos0 + qi + 1 - a.window) : 0;
+  // of the wave's rows: all attend inside [all_low, all_lim), none outside
+  // [any_low, any_lim); the workgroup's tokens
+  const int q_first = (tile * kChunkRows + wave * 32) / G;
+  const int q_last = min((tile * kChunkRows + wave * 32 + 31) / G, sq.rows - 1);
+  const int all_lim = min(pos0 + q_first + 1, sq.len);
+  const int any_lim = q_first < sq.rows ? min(pos0 + q_last + 1, sq.len) : 0;
+  const int all_low = a.window > 0 ? max(0, pos0 + q_last + 1 - a.window) : 0;
+  const int any_low = a.window > 0 ? max(0, pos0 + q_first + 1 - a.window) : 0;
+  const int wg_first = tile * kChunkRows / G;
+  const int wg_last = min((tile * kChunkRows + kChunkRows - 1) / G, sq.rows - 1);
+  int t0 = span.begin + part * span.each;
+  const int t1 = min(min(span.end, t0 + span.each), pos0 + wg_last + 1);
+  if (a.window > 0) t0 = max(t0, (pos0 + wg_first + 1 - a.window) & ~(kTok - 1));
+
+  uint32_t qreg[DP / 16][4];
+  {
+    const uint16_t *qp = a.q.data + (int64_t)(sq.row0 + (there ? qi : 0)) * a.q.row_stride +
+                         (int64_t)(h * G + r % G) * a.q.head_stride;
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+      const int d = k * 16 + gg * 8;
+      u32x4 v = {0, 0, 0, 0};
+      if (there && d < D) v = *reinterpret_cast<const u32x4 *>(qp + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qreg[k][i] = v[i];
+    }
+  }
+
+  // O is held in units of v_scale / owed: a wave that skips a tile owes O the
+  // change of the unit
+  float m = kNegInf, l = 0.f, v_scale = 0.f, owed = 1.f;
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+
+  const int64_t token_bytes = (int64_t)H * D * EB, half_piece = kv.piece >> 1;
+  const int chunk = tid % CH, first_tok = tid / CH;
+
+  // the next tile's keys and values on their way to LDS, and its scales (of
+  // token `lane`)
+  uint32_t kr[PASS][FP8 ? 2 : 4], vr[PASS][FP8 ? 2 : 4];
+  float k_sc = 0.f, v_sc = 0.f;
+  bool all_pages = true;
+  auto load = [&](int base) {
+    const int tok = base + lane;
+    int p = over_page(kv, tok);
+    const int slot0 = tok - p * T;
+    p = min(p, last_page);
+    const int page0 = table[p];
+    const bool ok = tok < sq.len && (uint32_t)page0 < (uint32_t)kv.num_pages;
+    const int page = ok ? page0 : 0, slot = ok ? slot0 : -1;
+    all_pages = __all(ok);
+    if (FP8) {
+      const float *sp = kv.scales + (int64_t)page * kv.scale_page + h * kv.scale_head;
+      k_sc = ok ? sp[0] * a.scale_log2 : 0.f;
+      v_sc = ok ? sp[kv.scale_kv] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < PASS; ++j) {
+      const int t = first_tok + j * STEP;
+      const int pg = __shfl(page, t), sl = __shfl(slot, t);
+      const uint8_t *src = kv.base + pg * kv.piece + max(sl, 0) * token_bytes +
+                           ((int64_t)h * D + (chunk * 8 < D ? chunk * 8 : 0)) * EB;
+      const bool in = sl >= 0 && chunk * 8 < D;
+      if constexpr (FP8) {
+        u32x2 x = *reinterpret_cast<const u32x2 *>(src);
+        u32x2 y = *reinterpret_cast<const u32x2 *>(src + half_piece);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          kr[j][i] = in ? x[i] : 0;
+          vr[j][i] = in ? y[i] : 0;
+        }
+      } else {
+        u32x4 x = *reinterpret_cast<const u32x4 *>(src);
+        u32x4 y = *reinterpret_cast<const u32x4 *>(src + half_piece);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          kr[j][i] = in ? x[i] : 0;
+          vr[j][i] = in ? y[i] : 0;
+        }
+      }
+    }
+  };
+
+  if (t0 < t1) load(t0);
+  for (int base = t0; base < t1; base += kTok) {
+    __syncthreads();  // the last tile has been read
+    if (FP8) {
+      float top = fabsf(v_sc);
+      for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+      top = fmaxf(top, v_scale);
+      if (top > v_scale) owed *= v_scale / top;
+      v_scale = top;
+      if (wave == 0) {
+        ks_lds[lane] = k_sc;
+        vs_lds[lane] = v_sc == 0.f ? 0.f : v_sc / v_scale;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < PASS; ++j) {
+      const int t = first_tok + j * STEP;
+      u32x4 x, y;
+      if constexpr (FP8) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[2 * i] = fp8_pair<ACT, false>(kr[j][i]);
+          x[2 * i + 1] = fp8_pair<ACT, true>(kr[j][i]);
+          y[2 * i] = fp8_pair<PV, false>(vr[j][i]);
+          y[2 * i + 1] = fp8_pair<PV, true>(vr[j][i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = kr[j][i];
+          y[i] = vr[j][i];
+        }
+      }
+      *reinterpret_cast<u32x4 *>(k_lds + t * KP + chunk * 16) = x;
+      *reinterpret_cast<u32x4 *>(v_lds + t * VP + chunk * 16) = y;
+    }
+    const bool whole = all_pages;
+    __syncthreads();
+    if (base + kTok < t1) load(base + kTok);
+    if (base >= any_lim || base + kTok <= any_low) continue;
+
+    f32x16 x[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        const u32x4 af =
+            *reinterpret_cast<const u32x4 *>(k_lds + (t * 32 + c) * KP + k * 32 + gg * 16);
+        x[t] = mfma32<ACT>(af, u32x4{qreg[k][0], qreg[k][1], qreg[k][2], qreg[k][3]}, x[t]);
+      }
+    }
+    if (FP8) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 f = *reinterpret_cast<const f32x4 *>(ks_lds + t * 32 + q * 8 + gg * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[t][q * 4 + i] *= f[i];
+        }
+    }
+    const float unit = FP8 ? 1.f : a.scale_log2;  // of a score, in powers of two
+    if (!(whole && base >= all_low && base + kTok <= all_lim)) {
+      // a page that is not there: its tokens' bits of `gone`
+      const int tok = base + lane;
+      const int pg = table[min(over_page(kv, tok), last_page)];
+      const uint64_t gone = __ballot((uint32_t)pg >= (uint32_t)kv.num_pages);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = t * 32 + (i >> 2) * 8 + gg * 4 + (i & 3);
+          if (base + at < low || base + at >= lim || ((gone >> at) & 1)) x[t][i] = kNegInf;
+        }
+    }
+    float top = m;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+    top = max_rows32(top);
+    const float ref = top == kNegInf ? 0.f : top * unit - kShift;
+    if (__any(top != m) || owed != 1.f) {
+      const float f = m == kNegInf ? 0.f : exp2_fast(m * unit - kShift - ref);
+      l *= f;
+      const float fo = f * owed;
+      owed = 1.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] *= fo;
+      m = top;
+    }
+    u32x4 pf[4];  // 16 tokens each
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = exp2_fast(x[t][q * 4 + i] * unit - ref);
+          l += p[i];
+        }
+        if (FP8) {
+          const f32x4 f = *reinterpret_cast<const f32x4 *>(vs_lds + t * 32 + q * 8 + gg * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] *= f[i];
+        }
+        pf[t * 2 + (q >> 1)][(q & 1) * 2] = pack_act<PV>(p[0], p[1]);
+        pf[t * 2 + (q >> 1)][(q & 1) * 2 + 1] = pack_act<PV>(p[2], p[3]);
+      }
+    // lane of 16: token (lane / 4) and four elements of 16 of a transposing
+    // read; it gets one element of four tokens
+    const uint8_t *vp =
+        v_lds + (gg * 4 + ((lane & 15) >> 2)) * VP + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint8_t *p = vp + k * 16 * VP + dt * 64;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * VP));
+        const u32x2 x0 = __builtin_bit_cast(u32x2, lo), x1 = __builtin_bit_cast(u32x2, hi);
+        o[dt] = mfma32<PV>(u32x4{x0[0], x0[1], x1[0], x1[1]}, pf[k], o[dt]);
+      }
+  }
+
+  const float total = add_rows32(l);
+  if (!there) return;
+  const float unit = FP8 ? 1.f : a.scale_log2;
+  const float ref = m == kNegInf ? kNegInf : m * unit - kShift;
+  const int64_t row = sq.row0 + qi, head = h * G + r % G;
+  const float out_scale = FP8 ? v_scale * owed : 1.f;
+  if (span.parts == 1) {
+    const float f = total == 0.f ? 0.f : out_scale / total;
+    uint16_t *op = a.out.data + row * a.out.row_stride + head * a.out.head_stride;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int d = dt * 32 + q * 8 + gg * 4;
+        if (d >= D) continue;
+        *reinterpret_cast<u32x2 *>(op + d) =
+            u32x2{pack_act<ACT>(o[dt][q * 4] * f, o[dt][q * 4 + 1] * f),
+                  pack_act<ACT>(o[dt][q * 4 + 2] * f, o[dt][q * 4 + 3] * f)};
+      }
+    if (a.lse && gg == 0)
+      a.lse[row * H * G + head] =
+          total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+  } else {
+    const int64_t at = (row * H * G + head) * a.splits + part;
+    float *op = a.part_o + at * D;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int d = dt * 32 + q * 8 + gg * 4;
+        if (d >= D) continue;
+        *reinterpret_cast<f32x4 *>(op + d) =
+            f32x4{o[dt][q * 4] * out_scale, o[dt][q * 4 + 1] * out_scale,
+                  o[dt][q * 4 + 2] * out_scale, o[dt][q * 4 + 3] * out_scale};
+      }
+    if (gg == 0) {
+      a.part_ml[at * 2] = ref;
+      a.part_ml[at * 2 + 1] = total;
+    }
+  }
+}
+
+template <int ACT, bool FP8>
+hipError_t dims(const AttendArgs &a, hipStream_t s) {
+  const int64_t tiles = ((int64_t)a.b.max_rows * a.group + kChunkRows - 1) / kChunkRows;
+  const dim3 grid((unsigned)(a.b.n_seqs * tiles * a.splits * a.kv.heads)), block(kThreads);
+  if (a.kv.head_dim <= 64)
+    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 2>), grid, block, 0, s, a);
+  else if (a.kv.head_dim <= 128)
+    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 4>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 8>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend_chunk(const AttendArgs &a, int act, int fp8, hipStream_t s) {
+  (void)hipGetLastError();
+  if (act == kBf16) return fp8 ? dims<kBf16, true>(a, s) : dims<kBf16, false>(a, s);
+  return fp8 ? dims<kF16, true>(a, s) : dims<kF16, false>(a, s);
+}
+
+}  // namespace ea

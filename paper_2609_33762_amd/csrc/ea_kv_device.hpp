@@ -1,0 +1,187 @@
+// Device helpers of the cache operators' kernels (gfx950).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "ea_kv_ops.hpp"
+
+namespace ea {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kLanes = 64;
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int32_t uniform(int32_t v) {
+  return (int32_t)__builtin_amdgcn_readfirstlane((uint32_t)v);
+}
+__device__ inline float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
+__device__ inline int32_t over_page(const KvLayer &kv, int32_t token) {
+  return (int32_t)(((uint64_t)(uint32_t)token * kv.t_mul) >> kv.t_shift);
+}
+
+// First row and rows of a sequence, both held to the batch's bounds, and its
+// cached tokens.
+struct Seq {
+  int32_t row0, rows, len;
+};
+__device__ inline Seq sequence(const BatchRows &b, int32_t s) {
+  Seq q;
+  if (b.row_start) {
+    const int32_t lo = min(max(b.row_start[s], 0), b.n_rows);
+    const int32_t hi = min(max(b.row_start[s + 1], lo), b.n_rows);
+    q.row0 = lo;
+    q.rows = min(hi - lo, b.max_rows);
+  } else {
+    q.row0 = s;
+    q.rows = s < b.n_rows ? 1 : 0;
+  }
+  q.len = min(max(b.kv_len[s], 0), b.max_kv);
+  return q;
+}
+
+// The sequence of a row: the last one that starts at or before it.
+__device__ inline int32_t sequence_of_row(const BatchRows &b, int32_t row) {
+  if (!b.row_start) return row;
+  int32_t lo = 0, hi = b.n_seqs - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (b.row_start[mid] <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// The tokens [begin, end) that any row of a sequence attends to, counted
+// along the selection where there is one, and the parts of `each` tokens they
+// are split into.
+struct Span {
+  int32_t begin, end, each, parts;
+};
+__device__ inline Span span_of(const AttendArgs &a, const Seq &q, int32_t pos) {
+  Span s;
+  if (a.selected) {  // `pos` is the row's own
+    s.begin = 0;
+    s.end = pos < 0 ? 0 : min(a.budget, over_page(a.kv, pos) + 1) * a.kv.page_tokens;
+  } else {
+    const int32_t lowest = q.len - q.rows + 1 - a.window;
+    s.begin = a.window > 0 && lowest > 0 ? lowest & ~(kChunkTokens - 1) : 0;
+    s.end = q.len;
+  }
+  s.each = !a.selected && q.rows * a.group > a.split_rows_most ? a.chunk_tokens : a.split_tokens;
+  s.parts = max(1, (s.end - s.begin + s.each - 1) / s.each);
+  return s;
+}
+
+// Largest value over the lanes that hold the same column of a 16-column
+// (l, l ^ 16, l ^ 32, l ^ 48) or 32-column (l, l ^ 32) tile.
+__device__ inline float max_rows32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return max_rows32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float add_rows32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline float add_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return add_rows32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// The smallest power of two s >= 2^-126 with top * s >= amax, top = 448 (fp8
+// e4m3) or 127 (whole numbers of 8 bits): from the bits, exact.
+__device__ inline float power_for(float amax, uint32_t mantissa_top, int32_t log2_top) {
+  const uint32_t u = __float_as_uint(amax);
+  int32_t e = (int32_t)(u >> 23) - log2_top + ((u & 0x7fffff) > mantissa_top ? 1 : 0);
+  // biased exponent of s; a subnormal or zero amax ends at the smallest
+  e = min(max(e, 1), 254);
+  return __uint_as_float((uint32_t)e << 23);
+}
+__device__ inline float fp8_scale(float amax) { return power_for(amax, 0x600000, 8); }
+__device__ inline float int8_scale(float amax) { return power_for(amax, 0x7e0000, 6); }
+// 1 / s of a power of two s in [2^-126, 2^127]; 2^-127 as a subnormal.
+__device__ inline float power_inverse(float s) {
+  const int32_t e = 254 - (int32_t)(__float_as_uint(s) >> 23);
+  return e > 0 ? __uint_as_float((uint32_t)e << 23) : __uint_as_float(0x400000);
+}
+
+__device__ inline bool finite(float v) { return (__float_as_uint(v) & 0x7f800000) != 0x7f800000; }
+
+template <int ACT>
+struct ActOf;
+template <>
+struct ActOf<kBf16> {
+  typedef __bf16 T;
+  typedef bf16x8 V8;
+};
+template <>
+struct ActOf<kF16> {
+  typedef _Float16 T;
+  typedef f16x8 V8;
+};
+
+template <int ACT>
+__device__ inline float act_to_float(uint16_t v) {
+  return (float)__builtin_bit_cast(typename ActOf<ACT>::T, v);
+}
+template <int ACT>
+__device__ inline uint16_t float_to_act(float v) {
+  return __builtin_bit_cast(uint16_t, (typename ActOf<ACT>::T)v);
+}
+template <int ACT>
+__device__ inline uint32_t pack_act(float lo, float hi) {
+  return (uint32_t)float_to_act<ACT>(lo) | ((uint32_t)float_to_act<ACT>(hi) << 16);
+}
+
+// Two fp8 codes (the low or high half of w) as two 16-bit values, exact.
+template <int ACT, bool HIGH>
+__device__ inline uint32_t fp8_pair(uint32_t w) {
+  if constexpr (ACT == kBf16)
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+}
+
+template <int ACT>
+__device__ inline f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+  if constexpr (ACT == kBf16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <int ACT>
+__device__ inline f32x16 mfma32(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
+  if constexpr (ACT == kBf16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+__device__ inline float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+}  // namespace ea

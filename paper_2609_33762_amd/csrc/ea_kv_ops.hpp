@@ -1,0 +1,106 @@
+// Shared declarations of the cache operators (append, attention, block
+// selection): kernel arguments and launchers.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace ea {
+
+enum Act : int32_t { kBf16 = 0, kF16 = 1 };
+
+// One layer of the paged cache, [P][2][T][H][D], and its planes.
+struct KvLayer {
+  uint8_t *base;          // first byte of the layer
+  float *scales;          // first scale of the layer (fp8), or nullptr
+  int8_t *bounds;         // [P][2][H][D] lowest, highest; or nullptr
+  float *bound_scales;    // [P][H]
+  int64_t piece;          // bytes of one page
+  int32_t num_pages, page_tokens, heads, head_dim;
+  int32_t scale_page, scale_kv, scale_head;  // strides of `scales` in floats
+  // token / page_tokens for 0 <= token < 2^31: (token * t_mul) >> t_shift
+  uint32_t t_mul;
+  int32_t t_shift;
+};
+
+// The sequences of one call; every array is device memory.
+struct BatchRows {
+  const int32_t *page_table;  // [n_seqs][table_stride]
+  const int32_t *kv_len;      // [n_seqs]
+  const int32_t *row_start;   // [n_seqs + 1], or nullptr: one row each
+  int64_t table_stride;
+  int32_t n_seqs, n_rows, max_rows, max_kv;
+};
+
+// Rows of heads: element (row, head, d) at row * row_stride + head *
+// head_stride + d of 16-bit elements.
+struct HeadRows {
+  uint16_t *data;
+  int64_t row_stride, head_stride;
+};
+
+struct AppendArgs {
+  KvLayer kv;
+  BatchRows b;
+  HeadRows k, v, q, q_out;  // q.data null: no queries
+  const float *rope;        // [rope_len][rope_dim]: cosines, then sines; or nullptr
+  int32_t rope_dim, interleaved;
+  int32_t q_heads;
+  int32_t fp8;
+  int32_t pages_most;       // pages one sequence's new tokens can touch
+};
+
+struct AttendArgs {
+  KvLayer kv;
+  BatchRows b;
+  HeadRows q, out;
+  float *lse;               // [n_rows][q_heads] or nullptr
+  const int32_t *selected;  // [n_rows][H][budget] or nullptr
+  int32_t budget;
+  int32_t window;
+  int32_t group;            // query heads per KV head
+  float scale_log2;         // softmax scale times log2(e)
+  // Sequences with at most this many rows times heads of a group go to the
+  // split kernel, others to the chunk kernel.
+  int32_t split_rows_most;
+  // Work along a sequence's tokens comes in parts of split_tokens (split
+  // kernel) or chunk_tokens (chunk kernel), `splits` of them at most; the
+  // parts of one row are joined from the workspace.
+  int32_t splits, split_tokens, chunk_tokens;
+  float *part_o;            // [n_rows][q_heads][splits][head_dim]
+  float *part_ml;           // [n_rows][q_heads][splits][2]
+};
+
+struct SelectArgs {
+  KvLayer kv;
+  BatchRows b;
+  HeadRows q;
+  int32_t *selected;        // [n_rows][H][budget]
+  uint32_t *keys;           // [n_rows][H][blocks_most] ordered scores
+  int32_t budget, first, last;
+  int32_t group;
+  int32_t blocks_most;      // blocks of max_kv tokens
+  int32_t blocks_wave;      // blocks one wave scores
+};
+
+constexpr int32_t kMaxHeadDim = 256;
+constexpr int32_t kMaxSelectBlocks = 65536;
+
+// Most query rows times heads of a group that the split kernel takes (its
+// columns per wave); heads wider than 128 leave it fewer registers.
+constexpr int32_t split_rows_cap(int32_t head_dim) { return head_dim > 128 ? 16 : 64; }
+
+// Tokens a step of the split kernel covers and rows of a chunk workgroup.
+constexpr int32_t kSplitStep = 32;
+constexpr int32_t kChunkRows = 128;
+constexpr int32_t kChunkTokens = 64;
+
+hipError_t launch_append(const AppendArgs &a, int act, hipStream_t s);
+hipError_t launch_bounds(const KvLayer &kv, int act, int fp8, int32_t layers, int64_t layer_bytes,
+                         int64_t layer_scales, const int32_t *pages, int32_t n, hipStream_t s);
+hipError_t launch_attend_split(const AttendArgs &a, int act, int fp8, hipStream_t s);
+hipError_t launch_attend_chunk(const AttendArgs &a, int act, int fp8, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs &a, int act, hipStream_t s);
+hipError_t launch_select(const SelectArgs &a, int act, hipStream_t s);
+
+}  // namespace ea
