@@ -664,7 +664,9 @@ typedef struct {
  * attends to nothing gets zeros.  What lies in slots that no row of the
  * sequence attends to never matters.  workspace (16-byte aligned device
  * memory, ea_attend_workspace bytes; NULL when that is 0) is scratch of this
- * call: calls that may overlap need their own. */
+ * call: calls that may overlap need their own.  Its first 32 KiB hold
+ * counters: zero when it is first used, left zero by every call, and nobody
+ * else's in between. */
 int64_t ea_attend_workspace(const ea_cache *cache, const ea_batch *batch,
                             const ea_attention *args);
 int ea_attend(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,

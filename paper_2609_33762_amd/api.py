@@ -220,7 +220,7 @@ class Cache:
             N.check("ea_attend_workspace", need)
         N.check("ea_attend", lib.ea_attend(
             self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
-            batch.workspace(need, s), need, s))
+            batch.workspace("attend", need, s), need, s))
 
     def select_blocks(self, layer, batch, q, selected, first=1, last=1, stream=None):
         """Blocks for sparse attention of q's rows from the bounds planes:
@@ -238,7 +238,7 @@ class Cache:
             N.check("ea_select_workspace", need)
         N.check("ea_select_blocks", lib.ea_select_blocks(
             self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
-            batch.workspace(need, s), need, s))
+            batch.workspace("select", need, s), need, s))
 
 
 _ACT = {"torch.bfloat16": N.EA_BF16, "torch.float16": N.EA_F16}
@@ -302,21 +302,22 @@ class Batch:
                                 max_rows, max_kv)
         self._scratch = {}
 
-    def workspace(self, nbytes, stream):
-        """Device scratch of at least nbytes for calls on this stream."""
+    def workspace(self, call, nbytes, stream):
+        """Device scratch of at least nbytes for this call on this stream,
+        zero when it is new."""
         import torch
         if nbytes == 0:
             return None
-        t = self._scratch.get(stream)
+        t = self._scratch.get((call, stream))
         if t is None or t.numel() < nbytes:
             # taken on the calls' own stream: the allocator orders reuse by it
             if stream == current_stream():
-                t = torch.empty(nbytes, dtype=torch.uint8, device=self.kv_len.device)
+                t = torch.zeros(nbytes, dtype=torch.uint8, device=self.kv_len.device)
             else:
                 s = torch.cuda.ExternalStream(stream, device=self.kv_len.device)
                 with torch.cuda.stream(s):
-                    t = torch.empty(nbytes, dtype=torch.uint8, device=self.kv_len.device)
-            self._scratch[stream] = t
+                    t = torch.zeros(nbytes, dtype=torch.uint8, device=self.kv_len.device)
+            self._scratch[call, stream] = t
         return t.data_ptr()
 
 

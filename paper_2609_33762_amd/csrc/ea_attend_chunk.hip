@@ -80,8 +80,8 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   const int any_low = a.window > 0 ? max(0, pos0 + q_first + 1 - a.window) : 0;
   const int wg_first = tile * kChunkRows / G;
   const int wg_last = min((tile * kChunkRows + kChunkRows - 1) / G, sq.rows - 1);
-  int t0 = span.begin + part * span.each;
-  const int t1 = min(min(span.end, t0 + span.each), pos0 + wg_last + 1);
+  int t0 = span.begin + part * a.chunk_tokens;
+  const int t1 = min(min(span.end, t0 + a.chunk_tokens), pos0 + wg_last + 1);
   if (a.window > 0) t0 = max(t0, (pos0 + wg_first + 1 - a.window) & ~(kTok - 1));
 
   uint32_t qreg[DP / 16][4];

@@ -30,7 +30,7 @@ __device__ inline float uniform(float v) {
 }
 
 __device__ inline int32_t over_page(const KvLayer &kv, int32_t token) {
-  return (int32_t)(((uint64_t)(uint32_t)token * kv.t_mul) >> kv.t_shift);
+  return (int32_t)(__umulhi((uint32_t)token << 1, kv.t_mul) >> kv.t_shift);
 }
 
 // First row and rows of a sequence, both held to the batch's bounds, and its
@@ -66,10 +66,10 @@ __device__ inline int32_t sequence_of_row(const BatchRows &b, int32_t row) {
 }
 
 // The tokens [begin, end) that any row of a sequence attends to, counted
-// along the selection where there is one, and the parts of `each` tokens they
-// are split into.
+// along the selection where there is one, and the parts the chunk kernel
+// splits them into.
 struct Span {
-  int32_t begin, end, each, parts;
+  int32_t begin, end, parts;
 };
 __device__ inline Span span_of(const AttendArgs &a, const Seq &q, int32_t pos) {
   Span s;
@@ -81,8 +81,7 @@ __device__ inline Span span_of(const AttendArgs &a, const Seq &q, int32_t pos) {
     s.begin = a.window > 0 && lowest > 0 ? lowest & ~(kChunkTokens - 1) : 0;
     s.end = q.len;
   }
-  s.each = !a.selected && q.rows * a.group > a.split_rows_most ? a.chunk_tokens : a.split_tokens;
-  s.parts = max(1, (s.end - s.begin + s.each - 1) / s.each);
+  s.parts = max(1, (s.end - s.begin + a.chunk_tokens - 1) / a.chunk_tokens);
   return s;
 }
 

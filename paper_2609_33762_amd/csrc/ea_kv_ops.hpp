@@ -18,7 +18,8 @@ struct KvLayer {
   int64_t piece;          // bytes of one page
   int32_t num_pages, page_tokens, heads, head_dim;
   int32_t scale_page, scale_kv, scale_head;  // strides of `scales` in floats
-  // token / page_tokens for 0 <= token < 2^31: (token * t_mul) >> t_shift
+  // token / page_tokens for 0 <= token < 2^31: the high 32 bits of 2 * token *
+  // t_mul, >> t_shift
   uint32_t t_mul;
   int32_t t_shift;
 };
@@ -63,10 +64,16 @@ struct AttendArgs {
   // Sequences with at most this many rows times heads of a group go to the
   // split kernel, others to the chunk kernel.
   int32_t split_rows_most;
-  // Work along a sequence's tokens comes in parts of split_tokens (split
-  // kernel) or chunk_tokens (chunk kernel), `splits` of them at most; the
-  // parts of one row are joined from the workspace.
-  int32_t splits, split_tokens, chunk_tokens;
+  // Split kernel: a workgroup takes heads_wg (1 or 2) neighbouring KV heads.  A unit (a sequence and as many heads) is split so that
+  // the parts of all fit split_wgs workgroups where they can, a part having
+  // least_steps steps at least; split_grid workgroups are enough for that.
+  // Their parts, and the counts of a unit's parts done, zero between calls.
+  int32_t heads_wg, split_wgs, least_steps, split_grid;
+  float *split_parts;
+  int32_t *arrivals;
+  // Chunk kernel: work along a sequence's tokens in parts of chunk_tokens,
+  // `splits` of them at most; launch_attend_join joins a row's parts.
+  int32_t splits, chunk_tokens;
   float *part_o;            // [n_rows][q_heads][splits][head_dim]
   float *part_ml;           // [n_rows][q_heads][splits][2]
 };
@@ -82,6 +89,22 @@ struct SelectArgs {
   int32_t blocks_most;      // blocks of max_kv tokens
   int32_t blocks_wave;      // blocks one wave scores
 };
+
+
+// Columns of the split kernel's variant for this many; waves of a variant's
+// workgroups, and the workgroups of it that its registers let a compute unit
+// hold.
+constexpr int32_t split_columns(int32_t most) { return most <= 16 ? 16 : most <= 32 ? 32 : 64; }
+constexpr int32_t split_waves(int32_t head_dim, int32_t columns) {
+  return head_dim > 128 || columns > 32 ? 4 : 8;
+}
+constexpr int32_t split_resident(int32_t head_dim, int32_t columns) {
+  return head_dim <= 64 && columns <= 16 ? 2 : 1;
+}
+
+// Counters at the start of an attention workspace: a unit's parts done.  More
+// units than kSplitUnits are not split.
+constexpr int32_t kSplitUnits = 4096, kArrivals = 8192;
 
 constexpr int32_t kMaxHeadDim = 256;
 constexpr int32_t kMaxSelectBlocks = 65536;
