@@ -28,7 +28,7 @@ constexpr int kTok = kChunkTokens;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-template <int ACT, bool FP8, int DT>
+template <int ACT, bool FP8, int DT, bool TILES>
 __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(AttendArgs a) {
   constexpr int DP = DT * 32;
   constexpr int CH = DP / 8;                  // chunks of 8 elements of a head
@@ -107,67 +107,147 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
 
-  const int64_t token_bytes = (int64_t)H * D * EB, half_piece = kv.piece >> 1;
+  const uint32_t token_bytes = H * D * EB, head_at = h * D * EB, piece = (uint32_t)kv.piece;
   const int chunk = tid % CH, first_tok = tid / CH;
 
-  // the next tile's keys and values on their way to LDS, and its scales (of
-  // token `lane`)
+  // ---- a tile's keys and values on their way to LDS, and its scales.
+  // TILES: 16 tokens share a page, so each of a wave's passes reads one page,
+  // as a buffer whose end cuts off what no row attends to (it reads as zero);
+  // pages are looked up a tile ahead.  Otherwise lane t looks up token t.
+  constexpr uint32_t kPast = 0x80000000u;
+  constexpr int TP = kTok / 16;
   uint32_t kr[PASS][FP8 ? 2 : 4], vr[PASS][FP8 ? 2 : 4];
-  float k_sc = 0.f, v_sc = 0.f;
-  bool all_pages = true;
+  float k_sc[TILES ? TP : 1] = {}, v_sc[TILES ? TP : 1] = {};
+  uint32_t here[TP] = {};  // TILES: pages of the tile to load
+  uint64_t gone = 0;       // tokens of the loaded tile whose page is not there
+  uint32_t place[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    place[i] = chunk * 8 < D ? ((first_tok + i * 8) & 15) * token_bytes + chunk * 8 * EB : kPast;
+  auto look = [&](int base) {
+#pragma unroll
+    for (int t = 0; t < TP; ++t)
+      here[t] = table[(uint32_t)min(over_page(kv, base + t * 16), last_page)];
+  };
   auto load = [&](int base) {
-    const int tok = base + lane;
-    int p = over_page(kv, tok);
-    const int slot0 = tok - p * T;
-    p = min(p, last_page);
-    const int page0 = table[p];
-    const bool ok = tok < sq.len && (uint32_t)page0 < (uint32_t)kv.num_pages;
-    const int page = ok ? page0 : 0, slot = ok ? slot0 : -1;
-    all_pages = __all(ok);
-    if (FP8) {
-      const float *sp = kv.scales + (int64_t)page * kv.scale_page + h * kv.scale_head;
-      k_sc = ok ? sp[0] * a.scale_log2 : 0.f;
-      v_sc = ok ? sp[kv.scale_kv] : 0.f;
-    }
+    gone = 0;
+    if constexpr (TILES) {
+      uint32_t page[TP], page_of[TP];
 #pragma unroll
-    for (int j = 0; j < PASS; ++j) {
-      const int t = first_tok + j * STEP;
-      const int pg = __shfl(page, t), sl = __shfl(slot, t);
-      const uint8_t *src = kv.base + pg * kv.piece + max(sl, 0) * token_bytes +
-                           ((int64_t)h * D + (chunk * 8 < D ? chunk * 8 : 0)) * EB;
-      const bool in = sl >= 0 && chunk * 8 < D;
-      if constexpr (FP8) {
-        u32x2 x = *reinterpret_cast<const u32x2 *>(src);
-        u32x2 y = *reinterpret_cast<const u32x2 *>(src + half_piece);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          kr[j][i] = in ? x[i] : 0;
-          vr[j][i] = in ? y[i] : 0;
+      for (int t = 0; t < TP; ++t) {
+        page_of[t] = uniform(here[t]);
+        const bool ok = page_of[t] < (uint32_t)kv.num_pages;
+        page[t] = ok ? page_of[t] : 0;
+        if (!ok) gone |= 0xffffull << (16 * t);
+        if (FP8) {
+          const float *sp =
+              kv.scales + ((uint64_t)page[t] * (uint32_t)kv.scale_page + h * kv.scale_head);
+          k_sc[t] = sp[0];
+          v_sc[t] = ok && base + t * 16 < sq.len ? sp[kv.scale_kv] : 0.f;
         }
-      } else {
-        u32x4 x = *reinterpret_cast<const u32x4 *>(src);
-        u32x4 y = *reinterpret_cast<const u32x4 *>(src + half_piece);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          kr[j][i] = in ? x[i] : 0;
-          vr[j][i] = in ? y[i] : 0;
+      for (int j = 0; j < PASS; ++j) {
+        // the pass's 16 tokens, their page and place in it
+        const int t = DT == 2 ? (wave >> 1) + 2 * j : j * STEP / 16;
+        uint32_t pg = page[0];
+#pragma unroll
+        for (int i = 1; i < TP; ++i) pg = i == t ? page[i] : pg;
+        const int tok = base + t * 16;
+        const uint32_t at = uniform((tok - over_page(kv, tok) * T) * token_bytes + head_at);
+        const uint32_t held =
+            uniform((gone >> (16 * t)) & 1 ? 0 : min(max(sq.len - tok, 0), 16));
+        uint8_t *p = kv.base + ((uint64_t)uniform(pg) * piece + at);
+        const auto kbuf = __builtin_amdgcn_make_buffer_rsrc(p, 0, held * token_bytes, 0x20000);
+        const auto vbuf =
+            __builtin_amdgcn_make_buffer_rsrc(p + piece / 2, 0, held * token_bytes, 0x20000);
+        const uint32_t off = place[DT == 8 ? j & 1 : 0];
+        if constexpr (FP8) {
+          const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(kbuf, off, 0, 0);
+          const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(vbuf, off, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            kr[j][i] = x[i];
+            vr[j][i] = y[i];
+          }
+        } else {
+          const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(kbuf, off, 0, 0);
+          const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(vbuf, off, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            kr[j][i] = x[i];
+            vr[j][i] = y[i];
+          }
+        }
+      }
+    } else {
+      const int tok = base + lane;
+      int p = over_page(kv, tok);
+      const int slot0 = tok - p * T;
+      const uint32_t page0 = table[(uint32_t)min(p, last_page)];
+      const bool there_is = page0 < (uint32_t)kv.num_pages, ok = tok < sq.len && there_is;
+      const uint32_t page = ok ? page0 : 0;
+      const int slot = ok ? slot0 : -1;
+      gone = __ballot(!there_is);
+      if (FP8) {
+        const float *sp = kv.scales + (uint64_t)page * (uint32_t)kv.scale_page + h * kv.scale_head;
+        k_sc[0] = ok ? sp[0] : 0.f;
+        v_sc[0] = ok ? sp[kv.scale_kv] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < PASS; ++j) {
+        const int t = first_tok + j * STEP;
+        const uint32_t pg = __shfl(page, t);
+        const int sl = __shfl(slot, t);
+        const uint8_t *src = kv.base + ((uint64_t)pg * piece + max(sl, 0) * token_bytes + head_at +
+                                        (chunk * 8 < D ? chunk * 8 : 0) * EB);
+        const bool in = sl >= 0 && chunk * 8 < D;
+        if constexpr (FP8) {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(src);
+          const u32x2 y = *reinterpret_cast<const u32x2 *>(src + piece / 2);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            kr[j][i] = in ? x[i] : 0;
+            vr[j][i] = in ? y[i] : 0;
+          }
+        } else {
+          const u32x4 x = *reinterpret_cast<const u32x4 *>(src);
+          const u32x4 y = *reinterpret_cast<const u32x4 *>(src + piece / 2);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            kr[j][i] = in ? x[i] : 0;
+            vr[j][i] = in ? y[i] : 0;
+          }
         }
       }
     }
   };
 
-  if (t0 < t1) load(t0);
+  if (t0 < t1) {
+    if (TILES) look(t0);
+    load(t0);
+    if (TILES) look(t0 + kTok);
+  }
   for (int base = t0; base < t1; base += kTok) {
     __syncthreads();  // the last tile has been read
+    float ks[TP], vs[TP];  // TILES: of 16 tokens each; else in LDS
     if (FP8) {
-      float top = fabsf(v_sc);
-      for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      top = fmaxf(top, v_scale);
+      float top = v_scale;
+#pragma unroll
+      for (int t = 0; t < (TILES ? TP : 1); ++t) top = fmaxf(top, fabsf(v_sc[t]));
+      if (!TILES)
+        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
       if (top > v_scale) owed *= v_scale / top;
       v_scale = top;
-      if (wave == 0) {
-        ks_lds[lane] = k_sc;
-        vs_lds[lane] = v_sc == 0.f ? 0.f : v_sc / v_scale;
+      const float inv = top >= 0x1p-126f ? 1.f / top : 0.f;
+#pragma unroll
+      for (int t = 0; t < TP; ++t) {
+        ks[t] = k_sc[TILES ? t : 0] * a.scale_log2;
+        vs[t] = v_sc[TILES ? t : 0] * inv;
+      }
+      if (!TILES && wave == 0) {
+        ks_lds[lane] = ks[0];
+        vs_lds[lane] = vs[0];
       }
     }
 #pragma unroll
@@ -192,9 +272,12 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
       *reinterpret_cast<u32x4 *>(k_lds + t * KP + chunk * 16) = x;
       *reinterpret_cast<u32x4 *>(v_lds + t * VP + chunk * 16) = y;
     }
-    const bool whole = all_pages;
+    const uint64_t gone_here = gone;
     __syncthreads();
-    if (base + kTok < t1) load(base + kTok);
+    if (base + kTok < t1) {
+      load(base + kTok);
+      if (TILES) look(base + 2 * kTok);
+    }
     if (base >= any_lim || base + kTok <= any_low) continue;
 
     f32x16 x[2];
@@ -209,28 +292,33 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
         x[t] = mfma32<ACT>(af, u32x4{qreg[k][0], qreg[k][1], qreg[k][2], qreg[k][3]}, x[t]);
       }
     }
+    auto scale_of = [&](const float *lds, const float *own, int t, int q) {
+      if constexpr (TILES) {
+        const float f = own[t * 2 + (q >> 1)];
+        return f32x4{f, f, f, f};
+      } else {
+        return *reinterpret_cast<const f32x4 *>(lds + t * 32 + q * 8 + gg * 4);
+      }
+    };
     if (FP8) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const f32x4 f = *reinterpret_cast<const f32x4 *>(ks_lds + t * 32 + q * 8 + gg * 4);
+          const f32x4 f = scale_of(ks_lds, ks, t, q);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[t][q * 4 + i] *= f[i];
         }
     }
     const float unit = FP8 ? 1.f : a.scale_log2;  // of a score, in powers of two
-    if (!(whole && base >= all_low && base + kTok <= all_lim)) {
-      // a page that is not there: its tokens' bits of `gone`
-      const int tok = base + lane;
-      const int pg = table[min(over_page(kv, tok), last_page)];
-      const uint64_t gone = __ballot((uint32_t)pg >= (uint32_t)kv.num_pages);
+    if (gone_here || base < all_low || base + kTok > all_lim) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int at = t * 32 + (i >> 2) * 8 + gg * 4 + (i & 3);
-          if (base + at < low || base + at >= lim || ((gone >> at) & 1)) x[t][i] = kNegInf;
+          if (base + at < low || base + at >= lim || ((gone_here >> at) & 1))
+            x[t][i] = kNegInf;
         }
     }
     float top = m;
@@ -263,7 +351,7 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
           l += p[i];
         }
         if (FP8) {
-          const f32x4 f = *reinterpret_cast<const f32x4 *>(vs_lds + t * 32 + q * 8 + gg * 4);
+          const f32x4 f = scale_of(vs_lds, vs, t, q);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] *= f[i];
         }
@@ -328,16 +416,21 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   }
 }
 
+template <int ACT, bool FP8, int DT>
+void go(const AttendArgs &a, dim3 grid, dim3 block, hipStream_t s) {
+  if (a.kv.page_tokens % 16 == 0)
+    hipLaunchKernelGGL((attend_chunk<ACT, FP8, DT, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((attend_chunk<ACT, FP8, DT, false>), grid, block, 0, s, a);
+}
+
 template <int ACT, bool FP8>
 hipError_t dims(const AttendArgs &a, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.b.max_rows * a.group + kChunkRows - 1) / kChunkRows;
   const dim3 grid((unsigned)(a.b.n_seqs * tiles * a.splits * a.kv.heads)), block(kThreads);
-  if (a.kv.head_dim <= 64)
-    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 2>), grid, block, 0, s, a);
-  else if (a.kv.head_dim <= 128)
-    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 4>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((attend_chunk<ACT, FP8, 8>), grid, block, 0, s, a);
+  if (a.kv.head_dim <= 64) go<ACT, FP8, 2>(a, grid, block, s);
+  else if (a.kv.head_dim <= 128) go<ACT, FP8, 4>(a, grid, block, s);
+  else go<ACT, FP8, 8>(a, grid, block, s);
   return hipGetLastError();
 }
 

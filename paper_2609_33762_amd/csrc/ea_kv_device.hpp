@@ -150,7 +150,9 @@ __device__ inline uint16_t float_to_act(float v) {
 }
 template <int ACT>
 __device__ inline uint32_t pack_act(float lo, float hi) {
-  return (uint32_t)float_to_act<ACT>(lo) | ((uint32_t)float_to_act<ACT>(hi) << 16);
+  typedef typename ActOf<ACT>::T V2 __attribute__((ext_vector_type(2)));
+  const V2 v = {(typename ActOf<ACT>::T)lo, (typename ActOf<ACT>::T)hi};  // one instruction
+  return __builtin_bit_cast(uint32_t, v);
 }
 
 // Two fp8 codes (the low or high half of w) as two 16-bit values, exact.
