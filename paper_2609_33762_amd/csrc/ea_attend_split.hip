@@ -129,17 +129,6 @@ __device__ inline void join_parts(const AttendArgs &a, int w0, int stride, int p
   }
 }
 
-// Sum over a lane and those below it.
-__device__ inline int scan_wave(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
-  return v;
-}
-
 // The work of a call in steps of 32 tokens for each run of a workgroup: a
 // sequence has `units` units (heads_wg KV heads; with selections, a row and
 // its KV head) of `steps` steps each.  Every wave of every workgroup finds the same totals from the

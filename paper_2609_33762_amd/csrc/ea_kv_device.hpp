@@ -108,6 +108,17 @@ __device__ inline float add_rows16(float v) {
   return add_rows32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Sum over a lane and those below it.
+__device__ inline int scan_wave(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return v;
+}
+
 // The smallest power of two s >= 2^-126 with top * s >= amax, top = 448 (fp8
 // e4m3) or 127 (whole numbers of 8 bits): from the bits, exact.
 __device__ inline float power_for(float amax, uint32_t mantissa_top, int32_t log2_top) {

@@ -272,7 +272,7 @@ int check_selection(const ea_cache *c, const ea_batch *b, const ea_selection *a)
   const int64_t blocks = ((int64_t)b->max_kv + d.page_tokens - 1) / d.page_tokens;
   if (blocks > ea::kMaxSelectBlocks || a->budget > ea::kMaxSelectBlocks) return EA_ENOTSUP;
   if ((int64_t)b->n_seqs * b->max_rows > INT32_MAX / d.num_kv_heads) return EA_ENOTSUP;
-  if ((int64_t)b->n_seqs * b->max_rows * d.num_kv_heads > INT32_MAX / (blocks / 64 + 1))
+  if ((int64_t)b->n_seqs * b->max_rows * d.num_kv_heads > INT32_MAX / (blocks / 16 + 1))
     return EA_ENOTSUP;
   return EA_OK;
 }
@@ -428,10 +428,11 @@ int ea_select_blocks(ea_cache *c, const ea_cache_planes *planes, int32_t layer,
   k.last = a->last;
   k.group = a->q_heads / d.num_kv_heads;
   k.blocks_most = (int32_t)(((int64_t)b->max_kv + d.page_tokens - 1) / d.page_tokens);
-  // about 4,096 waves, each with 64 blocks at least
+  // about 16,384 waves (contexts differ in length), each with 16 blocks at
+  // least: 64 rows, 4 heads and up to 4,096 blocks 47 us, with 4,096 waves 55
   const int64_t rows_heads = (int64_t)b->n_seqs * b->max_rows * d.num_kv_heads;
   k.blocks_wave = (int32_t)std::max<int64_t>(
-      64, up((rows_heads * k.blocks_most + 4095) / 4096, 16));
+      16, up((rows_heads * k.blocks_most + 16383) / 16384, 16));
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());
   KV_HIP(ea::launch_select(k, a->dtype, stream));

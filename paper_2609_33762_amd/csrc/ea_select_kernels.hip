@@ -25,10 +25,22 @@ __device__ inline uint32_t order_key(float v) {
 }
 constexpr uint32_t kAlways = 0xffffffffu;
 
+// Largest value over the 16 lanes of a row.
+__device__ inline float max_columns(float v) {
+  auto with = [&](auto moved) { v = fmaxf(v, __uint_as_float(moved)); };
+  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x128, 0xf, 0xf, true));  // row_ror:8
+  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x124, 0xf, 0xf, true));
+  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x122, 0xf, 0xf, true));
+  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x121, 0xf, 0xf, true));
+  return v;
+}
+
 // One wave: blocks_wave blocks of one query row and KV head.  The bounds of
-// 16 blocks are the rows of a product, the heads of the group its columns;
-// reading the bounds is what it costs.
-template <int ACT>
+// 16 blocks are the rows of a product, the heads of the group its columns.
+// Reading the bounds is what it costs: the next 16 load while these are
+// scored, and their pages were looked up before that.  KS: products of 64
+// elements a half.
+template <int ACT, int KS, bool WIDE>
 __global__ __launch_bounds__(kWaves *kLanes) void block_scores(SelectArgs a) {
   const KvLayer &kv = a.kv;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -51,10 +63,40 @@ __global__ __launch_bounds__(kWaves *kLanes) void block_scores(SelectArgs a) {
   const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
   uint32_t *keys = a.keys + ((int64_t)row * H + h) * a.blocks_most;
 
-  constexpr int KS = kMaxHeadDim / 64;  // products a half, at most
-  const int ks = (D + 63) / 64;
+  struct Bounds {
+    u32x4 x[KS][2];  // lowest, highest
+    float scale;
+    bool there;
+  };
+  auto page_of = [&](int b) { return (uint32_t)table[min(b + c, b1 - 1)]; };
+  auto load = [&](uint32_t pg) {
+    Bounds r;
+    r.there = pg < (uint32_t)kv.num_pages;
+    const uint32_t page = r.there ? pg : 0;
+    r.scale = kv.bound_scales[(uint64_t)page * H + h];
+    const int8_t *p = kv.bounds + ((uint64_t)page * 2 * H + h) * D;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        // past the head the query is zero: any bytes serve
+        const int d = k * 64 + g * 16;
+        const int8_t *ph = p + (int64_t)half * H * D;
+        if constexpr (WIDE) {
+          r.x[k][half] = *reinterpret_cast<const u32x4 *>(ph + (d < D ? d : 0));
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(ph + (d < D ? d : 0));
+          const u32x2 y = *reinterpret_cast<const u32x2 *>(ph + (d + 8 < D ? d + 8 : 0));
+          r.x[k][half] = u32x4{x[0], x[1], y[0], y[1]};
+        }
+      }
+    return r;
+  };
+
   for (int g0 = 0; g0 < G; g0 += 16) {  // 16 heads of the group at a time
     const int j = g0 + c;
+    uint32_t page = page_of(b0 + 16);
+    Bounds now = load(page_of(b0));
     // this column's query as whole numbers: elements k * 64 + g * 16 ..+15
     float q[KS][16];
     float amax = 0.f;
@@ -95,59 +137,52 @@ __global__ __launch_bounds__(kWaves *kLanes) void block_scores(SelectArgs a) {
         posv[k][w] = p;
       }
     for (int b = b0; b < b1; b += 16) {
-      const int mine = min(b + c, b1 - 1);
-      const int pg = table[mine];
-      const bool ok = (uint32_t)pg < (uint32_t)kv.num_pages;
-      const int page = ok ? pg : 0;
-      const int8_t *p = kv.bounds + ((int64_t)page * 2 * H + h) * D;
-      const float sb = kv.bound_scales[(int64_t)page * H + h];
+      const Bounds next = load(page);
+      page = page_of(b + 32);
       i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        if (k >= ks) break;
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {  // lowest, highest
-          const int8_t *ph = p + (int64_t)half * H * D;
-          const int d = k * 64 + g * 16;
-          u32x2 x = {0, 0}, y = {0, 0};  // past the head the query is zero
-          if (d < D) x = *reinterpret_cast<const u32x2 *>(ph + d);
-          if (d + 8 < D) y = *reinterpret_cast<const u32x2 *>(ph + d + 8);
+        for (int half = 0; half < 2; ++half)
           acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-              i32x4{(int)x[0], (int)x[1], (int)y[0], (int)y[1]},
+              __builtin_bit_cast(i32x4, now.x[k][half]),
               __builtin_bit_cast(i32x4, half ? posv[k] : neg[k]), acc, 0, 0, 0);
-        }
-      }
-      // result i: block b + g * 4 + i, head j
+      // result i: block b + g * 4 + i, head j; lane c < 4 writes block
+      // b + g * 4 + c
+      float best = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float block_scale = __shfl(sb, g * 4 + i);
-        const int block_there = __shfl((int)ok, g * 4 + i);
-        float v = j < G ? (float)acc[i] * sq_q * block_scale : kNegInf;
-        for (int d = 8; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-        const int blk = b + g * 4 + i;
-        if (c == i && blk < b1) {
-          uint32_t key = order_key(v);
-          if (g0) key = max(key, keys[blk]);
-          // always taken: the first blocks and the row's last ones; a page
-          // that is not there comes after every score
-          if (blk < a.first || blk >= held - a.last) key = kAlways;
-          else if (!block_there) key = 0;
-          keys[blk] = key;
-        }
+        const float v = max_columns(j < G ? (float)acc[i] * sq_q : kNegInf);
+        if (c == i) best = v;
       }
+      const int from = g * 4 + (c & 3), blk = b + from;
+      const float scale = __shfl(now.scale, from);
+      const int there = __shfl((int)now.there, from);
+      if (c < 4 && blk < b1) {
+        uint32_t key = order_key(best * scale);
+        if (g0) key = max(key, keys[blk]);
+        // always taken: the first blocks and the row's last ones; a page that
+        // is not there comes after every score
+        if (blk < a.first || blk >= held - a.last) key = kAlways;
+        else if (!there) key = 0;
+        keys[blk] = key;
+      }
+      now = next;
     }
   }
 }
 
-// One workgroup of 1024: the budget highest keys of a row and KV head, ties
-// to the lowest block, in the blocks' order.  The threads hold the keys in
-// registers (PER each); the smallest key taken is found from its highest
-// bits down, two at a time, by counting the keys not below three thresholds.
-template <int PER>
-__global__ __launch_bounds__(1024) void pick_blocks(SelectArgs a) {
-  __shared__ int32_t count[2][16][3];
-  __shared__ int32_t base_gt[16], base_eq[16];
-  const int H = a.kv.heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// One workgroup: the budget highest keys of a row and KV head, ties to the
+// lowest block, in the blocks' order; PER keys a thread.  The lowest key taken is found from its highest bits down: a
+// histogram of the eight highest bits in which the keys differ, then of the
+// next eight of those in the bin that the bound falls into, until a bin is
+// wanted as a whole.
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void pick_blocks(SelectArgs a) {
+  constexpr int W = THREADS / kLanes;
+  __shared__ int32_t count[W][4];
+  __shared__ int32_t bins[256], found[3];
+  const int H = a.kv.heads, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   uint32_t u = blockIdx.x;
   const int h = u % H;
   u /= H;
@@ -158,82 +193,153 @@ __global__ __launch_bounds__(1024) void pick_blocks(SelectArgs a) {
   const int held = pos < 0 ? 0 : over_page(a.kv, pos) + 1;
   int32_t *out = a.selected + ((int64_t)row * H + h) * a.budget;
   if (held <= a.budget) {  // all of them
-    for (int i = tid; i < a.budget; i += 1024) out[i] = i < held ? i : -1;
+    for (int i = tid; i < a.budget; i += THREADS) out[i] = i < held ? i : -1;
     return;
   }
   const uint32_t *keys = a.keys + ((int64_t)row * H + h) * a.blocks_most;
-  uint32_t key[PER];
+  // A place past the blocks holds 0, as does a block whose page is not there;
+  // scores are above that.
+  constexpr bool kHeld = PER <= 16;  // in registers; else read again
+  uint32_t kept[kHeld ? PER : 1];
+  auto fetch = [&](int i) {
+    const int b = (wave * PER + i) * kLanes + lane;
+    return b < held ? keys[b] : 0u;
+  };
+  if (kHeld) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = i * 1024 + tid;
-    key[i] = b < held ? keys[b] : 0;
+    for (int i = 0; i < PER; ++i) kept[kHeld ? i : 0] = fetch(i);
   }
-  uint32_t low = 0;  // at least `budget` keys are >= low
-  for (int bit = 30, turn = 0; bit >= 0; bit -= 2, turn ^= 1) {
-    int n[3] = {0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool there = i * 1024 + tid < held;
-#pragma unroll
-      for (int j = 0; j < 3; ++j)
-        n[j] += __popcll(__ballot(there && key[i] >= (low | ((uint32_t)(j + 1) << bit))));
-    }
-    if (lane == 0)
-#pragma unroll
-      for (int j = 0; j < 3; ++j) count[turn][wave][j] = n[j];
-    __syncthreads();
-    int total[3] = {0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < 16; ++w)
-#pragma unroll
-      for (int j = 0; j < 3; ++j) total[j] += count[turn][w][j];
-    uint32_t step = 0;
-#pragma unroll
-    for (int j = 0; j < 3; ++j)
-      if (total[j] >= a.budget) step = j + 1;
-    low |= step << bit;
-  }
-  // low is the budget-th highest key: all above it are taken, and the first
-  // of those equal to it
-  int above = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    above += __popcll(__ballot(i * 1024 + tid < held && key[i] > low));
-  __syncthreads();
-  if (lane == 0) count[0][wave][0] = above;
-  __syncthreads();
-  above = 0;
-#pragma unroll
-  for (int w = 0; w < 16; ++w) above += count[0][w][0];
-  const int equal_room = a.budget - above;
-  int gt_before = 0, eq_before = 0;  // over the rounds so far
+  auto key = [&](int i) { return kHeld ? kept[kHeld ? i : 0] : fetch(i); };
+  uint32_t any = 0, all = ~0u;
+  int forced = 0, scored = 0;
+#pragma unroll kHeld ? PER : 4
   for (int i = 0; i < PER; ++i) {
-    if (i * 1024 >= held) break;
-    const int b = i * 1024 + tid;
-    const uint32_t mine = b < held ? keys[b] : 0;
-    const bool gt = b < held && mine > low, eq = b < held && mine == low;
-    const uint64_t mg = __ballot(gt), me = __ballot(eq);
-    __syncthreads();
-    if (lane == 0) {
-      base_gt[wave] = __popcll(mg);
-      base_eq[wave] = __popcll(me);
+    const uint32_t k = key(i);
+    const bool plain = k != kAlways && k != 0;
+    if (plain) {
+      any |= k;
+      all &= k;
     }
-    __syncthreads();
-    int g0 = gt_before, e0 = eq_before;
-    for (int w = 0; w < 16; ++w) {
-      const int cg = base_gt[w], ce = base_eq[w];
-      if (w < wave) {
-        g0 += cg;
-        e0 += ce;
+    scored += __popcll(__ballot(plain));
+    forced += __popcll(__ballot(k == kAlways));
+  }
+  for (int d = 32; d; d >>= 1) {
+    any |= __shfl_xor(any, d);
+    all &= __shfl_xor(all, d);
+  }
+  if (lane == 0) {
+    count[wave][0] = (int32_t)any;
+    count[wave][1] = (int32_t)all;
+    count[wave][2] = scored;
+    count[wave][3] = forced;
+  }
+  if (tid < 256) bins[tid] = 0;
+  __syncthreads();
+  scored = forced = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    any |= (uint32_t)count[w][0];
+    all &= (uint32_t)count[w][1];
+    scored += count[w][2];
+    forced += count[w][3];
+  }
+  // low: keys above it are taken, and of those equal to it what there is room
+  // for
+  uint32_t low = 0;  // too few scores: all of them, then blocks without a page
+  int wanted = a.budget - forced;  // of the scored ones
+  if (wanted <= 0) {
+    low = kAlways;
+  } else if (wanted < scored) {
+    const uint32_t differ = any & ~all;
+    int bits = differ ? 32 - __builtin_clz(differ) : 0;  // still to be told apart
+    uint32_t prefix = bits < 32 ? all >> bits : 0;       // above them
+    while (bits > 0) {
+      const int width = min(bits, 8), shift = bits - width;
+#pragma unroll kHeld ? PER : 4
+      for (int i = 0; i < PER; ++i) {
+        const uint32_t k = key(i);
+        if (k != kAlways && k != 0 && (bits == 32 || k >> bits == prefix))
+          atomicAdd(&bins[(k >> shift) & ((1u << width) - 1)], 1);
       }
-      gt_before += cg;
-      eq_before += ce;
+      __syncthreads();
+      // keys in a bin or above it: thread t has bin 255 - t
+      const int in = tid < 256 ? bins[255 - tid] : 0;
+      const int upto = scan_wave(in);
+      if (lane == 63) count[wave][0] = upto;
+      __syncthreads();
+      if (tid < 256) {
+        bins[tid] = 0;
+        int from = upto;
+        for (int w = 0; w < wave; ++w) from += count[w][0];
+        if (from >= wanted && from - in < wanted) {
+          found[0] = 255 - tid;
+          found[1] = from - in;
+          found[2] = in;
+        }
+      }
+      __syncthreads();
+      prefix = (prefix << width) | (uint32_t)found[0];
+      wanted -= found[1];
+      bits = shift;
+      if (found[2] == wanted) break;
     }
-    const uint64_t below = (1ull << lane) - 1;
-    g0 += __popcll(mg & below);
-    e0 += __popcll(me & below);
-    if (gt || (eq && e0 < equal_room)) out[g0 + min(e0, equal_room)] = b;
+    // the keys from prefix << bits on, or that key itself with room for
+    // `wanted` of its blocks
+    low = prefix << bits;
+    if (bits > 0 && low > 0) --low;
   }
+  // Taken are the keys above low and the first of those equal to it that there
+  // is room for.  Wave w holds blocks w * PER * 64 on.
+  int gt = 0, eq = 0;
+#pragma unroll kHeld ? PER : 4
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t k = key(i);
+    gt += __popcll(__ballot(k > low));
+    eq += __popcll(__ballot(k == low && (wave * PER + i) * kLanes + lane < held));
+  }
+  __syncthreads();  // the last counts have been read
+  if (lane == 0) {
+    count[wave][0] = gt;
+    count[wave][1] = eq;
+  }
+  __syncthreads();
+  int above = 0, gt_at = 0, eq_at = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    above += count[w][0];
+    if (w < wave) {
+      gt_at += count[w][0];
+      eq_at += count[w][1];
+    }
+  }
+  const int room = a.budget - above;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll kHeld ? PER : 4
+  for (int i = 0; i < PER; ++i) {
+    const int b = (wave * PER + i) * kLanes + lane;
+    const uint32_t k = key(i);
+    const uint64_t mg = __ballot(k > low), me = __ballot(k == low && b < held);
+    const int g0 = gt_at + __popcll(mg & below), e0 = eq_at + __popcll(me & below);
+    if (b < held && (k > low || (k == low && e0 < room))) out[g0 + min(e0, room)] = b;
+    gt_at += __popcll(mg);
+    eq_at += __popcll(me);
+  }
+}
+
+template <int ACT, int KS>
+void scores_of(const SelectArgs &a, dim3 grid, dim3 block, hipStream_t s) {
+  // 16 elements at a time where heads are whole pieces of them
+  if (a.kv.head_dim % 16 == 0 && (reinterpret_cast<uintptr_t>(a.kv.bounds) & 15) == 0)
+    hipLaunchKernelGGL((block_scores<ACT, KS, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((block_scores<ACT, KS, false>), grid, block, 0, s, a);
+}
+
+template <int ACT>
+void scores(const SelectArgs &a, dim3 grid, dim3 block, hipStream_t s) {
+  if (a.kv.head_dim <= 64) scores_of<ACT, 1>(a, grid, block, s);
+  else if (a.kv.head_dim <= 128) scores_of<ACT, 2>(a, grid, block, s);
+  else scores_of<ACT, 4>(a, grid, block, s);
 }
 
 }  // namespace
@@ -243,14 +349,19 @@ hipError_t launch_select(const SelectArgs &a, int act, hipStream_t s) {
   const int64_t rows = (int64_t)a.b.n_seqs * a.b.max_rows * a.kv.heads;
   const int64_t waves = rows * ((a.blocks_most + a.blocks_wave - 1) / a.blocks_wave);
   const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(kWaves * kLanes);
-  if (act == kBf16) hipLaunchKernelGGL(block_scores<kBf16>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(block_scores<kF16>, grid, block, 0, s, a);
+  if (act == kBf16) scores<kBf16>(a, grid, block, s);
+  else scores<kF16>(a, grid, block, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 per_row((unsigned)rows), big(1024);
-  if (a.blocks_most <= 4 * 1024) hipLaunchKernelGGL(pick_blocks<4>, per_row, big, 0, s, a);
-  else if (a.blocks_most <= 16 * 1024) hipLaunchKernelGGL(pick_blocks<16>, per_row, big, 0, s, a);
-  else hipLaunchKernelGGL(pick_blocks<64>, per_row, big, 0, s, a);
+  const dim3 per_row((unsigned)rows);
+  if (a.blocks_most <= 256 * 4)
+    hipLaunchKernelGGL((pick_blocks<256, 4>), per_row, dim3(256), 0, s, a);
+  else if (a.blocks_most <= 256 * 16)
+    hipLaunchKernelGGL((pick_blocks<256, 16>), per_row, dim3(256), 0, s, a);
+  else if (a.blocks_most <= 1024 * 16)
+    hipLaunchKernelGGL((pick_blocks<1024, 16>), per_row, dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL((pick_blocks<1024, 64>), per_row, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
