@@ -97,6 +97,20 @@ __device__ inline float max_rows16(float v) {
                                                   false);
   return max_rows32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
+// A value of the lane CTRL - 0x120 below in a row of 16, around its end.
+template <int CTRL>
+__device__ inline float row_ror(float v) {
+  return __uint_as_float(
+      __builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// Largest value over the 16 lanes of a row; over all lanes.
+__device__ inline float max_columns(float v) {
+  v = fmaxf(v, row_ror<0x128>(v));
+  v = fmaxf(v, row_ror<0x124>(v));
+  v = fmaxf(v, row_ror<0x122>(v));
+  return fmaxf(v, row_ror<0x121>(v));
+}
+__device__ inline float max_wave(float v) { return max_rows16(max_columns(v)); }
 __device__ inline float add_rows32(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
                                                   false);

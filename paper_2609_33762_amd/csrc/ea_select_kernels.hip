@@ -25,16 +25,6 @@ __device__ inline uint32_t order_key(float v) {
 }
 constexpr uint32_t kAlways = 0xffffffffu;
 
-// Largest value over the 16 lanes of a row.
-__device__ inline float max_columns(float v) {
-  auto with = [&](auto moved) { v = fmaxf(v, __uint_as_float(moved)); };
-  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x128, 0xf, 0xf, true));  // row_ror:8
-  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x124, 0xf, 0xf, true));
-  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x122, 0xf, 0xf, true));
-  with(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x121, 0xf, 0xf, true));
-  return v;
-}
-
 // One wave: blocks_wave blocks of one query row and KV head.  The bounds of
 // 16 blocks are the rows of a product, the heads of the group its columns.
 // Reading the bounds is what it costs: the next 16 load while these are
