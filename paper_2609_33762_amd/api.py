@@ -94,13 +94,15 @@ class Cache:
                                      ("bound_scales", bound_scales, "torch.float32", blocks)):
             if t is None:
                 continue
-            if not t.is_cuda or not t.is_contiguous() or str(t.dtype) != dtype:
-                raise ValueError(f"{name} must be a contiguous {dtype} device tensor")
+            if t.device != kv.device or not t.is_contiguous() or str(t.dtype) != dtype:
+                raise ValueError(f"{name} must be a contiguous {dtype} tensor on kv's device")
             if t.numel() < need:
                 raise ValueError(f"{name} holds {t.numel()} values, the cache needs {need}")
         self.head_scales, self.bounds, self.bound_scales = head_scales, bounds, bound_scales
         self._planes = N.CachePlanes(*(None if t is None else t.data_ptr()
                                        for t in (head_scales, bounds, bound_scales)))
+        self._lib, self._planes_ref, self._device = lib, C.byref(self._planes), kv.device
+        self._shape = (num_kv_heads, head_dim, page_tokens, elem_bytes)
 
     @property
     def handle(self):
@@ -147,12 +149,27 @@ class Cache:
         N.check("ea_layer_checksum", N.load().ea_layer_checksum(
             self._h, layer, _ptr(p), len(p), d_out.data_ptr(), d_out.numel(), _stream(stream)))
 
-
     # ------------------------------------------------------ cache operators
     def _fits(self, batch):
         if batch.max_kv > batch.pages * self.page_tokens:
             raise ValueError(f"page_table holds {batch.pages} pages of {self.page_tokens} tokens "
                              f"a sequence, max_kv is {batch.max_kv}")
+        if batch.device != self._device:
+            raise ValueError("the batch lies on another device than the cache")
+
+    def _rows(self, t, what, n_rows, heads, act):
+        """Address and strides of rows [n_rows, heads, D]."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 3 or shape[0] < n_rows or shape[1] != heads or \
+                shape[2] != self.head_dim or stride[2] != 1 or t.device != self._device:
+            raise ValueError(f"{what} must be a tensor [{n_rows}, {heads}, {self.head_dim}] on the "
+                             "cache's device whose last dimension is contiguous")
+        if _dtype(t) != act:
+            raise ValueError(f"{what} must have the dtype of the call's other rows")
+        return t.data_ptr(), stride[0], stride[1]
+
+    def _stream(self, s):
+        return _current_raw(self._device.index) if s is None else _stream(s)
 
     def append_kv(self, layer, batch, k, v, rope=None, q=None, q_out=None, interleaved=False,
                   stream=None):
@@ -161,36 +178,32 @@ class Cache:
         by `rope` (float32 [positions, rope_dim], cosines then sines); q_out
         gets q rotated (it may be q)."""
         self._fits(batch)
-        act = _dtype(k)
-        if _dtype(v) != act:
-            raise ValueError("k and v must have one dtype")
-        a = N.Append(k=_rows(k, "k", batch.n_rows, self.num_kv_heads, self.head_dim),
-                     v=_rows(v, "v", batch.n_rows, self.num_kv_heads, self.head_dim),
-                     interleaved=int(interleaved), dtype=act)
+        act, n, heads = _dtype(k), batch.n_rows, self.num_kv_heads
+        a = N.Append(self._rows(k, "k", n, heads, act), self._rows(v, "v", n, heads, act))
         if q is not None:
-            if q_out is None or _dtype(q) != act or _dtype(q_out) != act:
-                raise ValueError("q needs a q_out, both of k's dtype")
-            a.q = _rows(q, "q", batch.n_rows, q.shape[1], self.head_dim)
-            a.q_out = _rows(q_out, "q_out", batch.n_rows, q.shape[1], self.head_dim)
-            a.q_heads = q.shape[1]
+            if q_out is None:
+                raise ValueError("q needs a q_out")
+            a.q_heads = heads = q.shape[1]
+            a.q = self._rows(q, "q", n, heads, act)
+            a.q_out = self._rows(q_out, "q_out", n, heads, act)
         if rope is not None:
-            if not rope.is_cuda or str(rope.dtype) != "torch.float32" or rope.dim() != 2 or \
+            if rope.device != self._device or rope.dtype not in _f32() or rope.dim() != 2 or \
                     not rope.is_contiguous():
-                raise ValueError("rope must be a contiguous float32 device matrix")
-            a.rope, a.rope_len, a.rope_dim = rope.data_ptr(), rope.shape[0], rope.shape[1]
-        N.check("ea_append_kv", N.load().ea_append_kv(
-            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
-            _stream(stream)))
+                raise ValueError("rope must be a contiguous float32 matrix on the cache's device")
+            a.rope, (a.rope_len, a.rope_dim) = rope.data_ptr(), rope.shape
+        a.interleaved, a.dtype = interleaved, act
+        N.check("ea_append_kv", self._lib.ea_append_kv(
+            self._h, self._planes_ref, layer, batch.ref, C.byref(a), self._stream(stream)))
 
     def bound_blocks(self, d_pages, layer_begin=0, layer_count=None, dtype=None, stream=None):
         """Bounds of whole blocks from their stored keys; d_pages: int32
         device tensor.  dtype: of a 16-bit cache (torch.bfloat16 if None)."""
-        _device_ints(d_pages, "d_pages")
+        _device_ints(d_pages, "d_pages", self._device)
         count = self.num_layers - layer_begin if layer_count is None else layer_count
-        act = N.EA_BF16 if dtype is None else _ACT[str(dtype)]
-        N.check("ea_bound_blocks", N.load().ea_bound_blocks(
-            self._h, C.byref(self._planes), layer_begin, count, d_pages.data_ptr(),
-            d_pages.numel(), act, _stream(stream)))
+        act = N.EA_BF16 if dtype is None else _act(dtype)
+        N.check("ea_bound_blocks", self._lib.ea_bound_blocks(
+            self._h, self._planes_ref, layer_begin, count, d_pages.data_ptr(), d_pages.numel(),
+            act, self._stream(stream)))
 
     def attend(self, layer, batch, q, out, scale=None, window=0, selected=None, lse=None,
                stream=None):
@@ -199,28 +212,32 @@ class Cache:
         last tokens only; selected int32 [n_rows, H, budget]: those blocks
         only (see select_blocks); lse: float32 [n_rows, q_heads] output."""
         self._fits(batch)
-        if _dtype(q) != _dtype(out):
-            raise ValueError("q and out must have one dtype")
-        a = N.Attention(q=_rows(q, "q", batch.n_rows, q.shape[1], self.head_dim),
-                        out=_rows(out, "out", batch.n_rows, q.shape[1], self.head_dim),
-                        window=window, q_heads=q.shape[1], dtype=_dtype(q),
-                        scale=self.head_dim ** -0.5 if scale is None else scale)
+        act, n, heads = _dtype(q), batch.n_rows, q.shape[1]
+        a = N.Attention(self._rows(q, "q", n, heads, act), self._rows(out, "out", n, heads, act))
+        budget = 0
         if selected is not None:
-            _selection(selected, batch.n_rows, self.num_kv_heads)
-            a.selected, a.budget = selected.data_ptr(), selected.shape[2]
+            budget = self._selection(selected, n)
+            a.selected, a.budget = selected.data_ptr(), budget
         if lse is not None:
-            if not lse.is_cuda or str(lse.dtype) != "torch.float32" or \
-                    not lse.is_contiguous() or tuple(lse.shape) != (batch.n_rows, q.shape[1]):
-                raise ValueError("lse must be a contiguous float32 device tensor "
-                                 "[n_rows, q_heads]")
+            if lse.device != self._device or lse.dtype not in _f32() or \
+                    not lse.is_contiguous() or tuple(lse.shape) != (n, heads):
+                raise ValueError("lse must be a contiguous float32 tensor [n_rows, q_heads] on "
+                                 "the cache's device")
             a.lse = lse.data_ptr()
-        lib, s = N.load(), _stream(stream)
-        need = lib.ea_attend_workspace(self._h, C.byref(batch.desc), C.byref(a))
-        if need < 0:
-            N.check("ea_attend_workspace", need)
-        N.check("ea_attend", lib.ea_attend(
-            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
-            batch.workspace("attend", need, s), need, s))
+        a.window, a.q_heads, a.dtype = window, heads, act
+        a.scale = self.head_dim ** -0.5 if scale is None else scale
+        ref, s = C.byref(a), self._stream(stream)
+        need = batch.need(("attend", self._shape, heads, window, budget),
+                          self._lib.ea_attend_workspace, self._h, ref)
+        N.check("ea_attend", self._lib.ea_attend(
+            self._h, self._planes_ref, layer, batch.ref, ref, batch.workspace("attend", need, s),
+            need, s))
+
+    def _selection(self, t, n_rows):
+        _device_ints(t, "selected", self._device)
+        if t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != self.num_kv_heads:
+            raise ValueError(f"selected must be [{n_rows}, {self.num_kv_heads}, budget]")
+        return t.shape[2]
 
     def select_blocks(self, layer, batch, q, selected, first=1, last=1, stream=None):
         """Blocks for sparse attention of q's rows from the bounds planes:
@@ -228,46 +245,53 @@ class Cache:
         table) of the highest-scored blocks in increasing order, the `first`
         blocks and the row's `last` ones always among them, -1 at the end."""
         self._fits(batch)
-        _selection(selected, batch.n_rows, self.num_kv_heads)
-        a = N.Selection(q=_rows(q, "q", batch.n_rows, q.shape[1], self.head_dim),
-                        selected=selected.data_ptr(), budget=selected.shape[2], first=first,
-                        last=last, q_heads=q.shape[1], dtype=_dtype(q))
-        lib, s = N.load(), _stream(stream)
-        need = lib.ea_select_workspace(self._h, C.byref(batch.desc), C.byref(a))
-        if need < 0:
-            N.check("ea_select_workspace", need)
-        N.check("ea_select_blocks", lib.ea_select_blocks(
-            self._h, C.byref(self._planes), layer, C.byref(batch.desc), C.byref(a),
-            batch.workspace("select", need, s), need, s))
+        act, heads, budget = _dtype(q), q.shape[1], self._selection(selected, batch.n_rows)
+        a = N.Selection(self._rows(q, "q", batch.n_rows, heads, act), selected.data_ptr(), budget,
+                        first, last, heads, act)
+        ref, s = C.byref(a), self._stream(stream)
+        need = batch.need(("select", self._shape, heads, budget, first, last),
+                          self._lib.ea_select_workspace, self._h, ref)
+        N.check("ea_select_blocks", self._lib.ea_select_blocks(
+            self._h, self._planes_ref, layer, batch.ref, ref, batch.workspace("select", need, s),
+            need, s))
 
 
-_ACT = {"torch.bfloat16": N.EA_BF16, "torch.float16": N.EA_F16}
+_ACT, _F32 = {}, []  # torch's dtypes, once a call has needed them
 
 
-def _dtype(t):
-    act = _ACT.get(str(t.dtype))
+def _act(dtype):
+    if not _ACT:
+        import torch
+        _ACT.update({torch.bfloat16: N.EA_BF16, torch.float16: N.EA_F16})
+    act = _ACT.get(dtype)
     if act is None:
-        raise ValueError(f"rows must be bfloat16 or float16, not {t.dtype}")
+        raise ValueError(f"rows must be bfloat16 or float16, not {dtype}")
     return act
 
 
-def _rows(t, what, n_rows, heads, head_dim):
-    if not t.is_cuda or t.dim() != 3 or t.shape[0] < n_rows or \
-            tuple(t.shape[1:]) != (heads, head_dim) or t.stride(2) != 1:
-        raise ValueError(f"{what} must be a device tensor [{n_rows}, {heads}, {head_dim}] "
-                         "whose last dimension is contiguous")
-    return N.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _dtype(t):
+    return _act(t.dtype)
 
 
-def _device_ints(t, what):
-    if not t.is_cuda or str(t.dtype) != "torch.int32" or not t.is_contiguous():
+def _f32():
+    if not _F32:
+        import torch
+        _F32.append(torch.float32)
+    return _F32
+
+
+def _current_raw(index):
+    """The handle of the current stream of a device, without the object
+    around it where torch gives it away."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(index).cuda_stream if raw is None else raw(index)
+
+
+def _device_ints(t, what, device=None):
+    if not t.is_cuda or str(t.dtype) != "torch.int32" or not t.is_contiguous() or \
+            (device is not None and t.device != device):
         raise ValueError(f"{what} must be a contiguous int32 device tensor")
-
-
-def _selection(t, n_rows, heads):
-    _device_ints(t, "selected")
-    if t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != heads:
-        raise ValueError(f"selected must be [{n_rows}, {heads}, budget]")
 
 
 class Batch:
@@ -281,14 +305,14 @@ class Batch:
         if not page_table.is_cuda or str(page_table.dtype) != "torch.int32" or \
                 page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be an int32 device matrix with contiguous rows")
-        _device_ints(kv_len, "kv_len")
+        _device_ints(kv_len, "kv_len", page_table.device)
         n = page_table.shape[0]
         if kv_len.numel() != n:
             raise ValueError("kv_len needs one length for each row of page_table")
         if row_start is None:
             n_rows, max_rows = n, min(n, 1)
         else:
-            _device_ints(row_start, "row_start")
+            _device_ints(row_start, "row_start", page_table.device)
             if row_start.numel() != n + 1:
                 raise ValueError("row_start needs one entry more than page_table has rows")
             if n_rows is None or max_rows is None:
@@ -300,23 +324,30 @@ class Batch:
                                 None if row_start is None else row_start.data_ptr(),
                                 page_table.stride(0) if n > 1 else self.pages, n, n_rows,
                                 max_rows, max_kv)
-        self._scratch = {}
+        self.ref, self.device = C.byref(self.desc), kv_len.device
+        self._need, self._scratch = {}, {}
+
+    def need(self, shape, query, cache, args):
+        """Workspace bytes of a call of this shape."""
+        n = self._need.get(shape)
+        if n is None:
+            n = query(cache, self.ref, args)
+            if n < 0:
+                N.check(query.__name__, n)
+            self._need[shape] = n
+        return n
 
     def workspace(self, call, nbytes, stream):
         """Device scratch of at least nbytes for this call on this stream,
         zero when it is new."""
-        import torch
         if nbytes == 0:
             return None
         t = self._scratch.get((call, stream))
         if t is None or t.numel() < nbytes:
+            import torch
             # taken on the calls' own stream: the allocator orders reuse by it
-            if stream == current_stream():
-                t = torch.zeros(nbytes, dtype=torch.uint8, device=self.kv_len.device)
-            else:
-                s = torch.cuda.ExternalStream(stream, device=self.kv_len.device)
-                with torch.cuda.stream(s):
-                    t = torch.zeros(nbytes, dtype=torch.uint8, device=self.kv_len.device)
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
+                t = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
             self._scratch[call, stream] = t
         return t.data_ptr()
 
