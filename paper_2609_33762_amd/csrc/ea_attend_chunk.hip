@@ -25,6 +25,9 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kLanes;
 constexpr int kTok = kChunkTokens;
 
+// Kinds of instructions for the scheduler, and key reads ahead of a product.
+constexpr int kValu = 0x2, kMfma = 0x8, kLdsRead = 0x100, kAhead = 4;
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -37,9 +40,9 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   constexpr int PV = FP8 ? kF16 : ACT;
   constexpr float kShift = PV == kF16 ? 15.f : 0.f;
   constexpr int EB = FP8 ? 1 : 2;
-  // pitches: eight tokens' 16 bytes of keys, and four tokens' 32 bytes of
-  // values, fall on different banks
-  constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32;
+  // pitches: sixteen tokens' 16 bytes of keys, and four tokens' 64 bytes of
+  // values, fall on different banks (of 64)
+  constexpr int KP = DP * 2 + 16, VP = DP * 2 + 64;
   __shared__ __align__(16) uint8_t k_lds[kTok * KP];
   __shared__ __align__(16) uint8_t v_lds[kTok * VP];
   __shared__ __align__(16) float ks_lds[kTok], vs_lds[kTok];
@@ -50,12 +53,16 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   const int H = kv.heads, D = kv.head_dim, T = kv.page_tokens, G = a.group;
   const int tiles_most = (a.b.max_rows * G + kChunkRows - 1) / kChunkRows;
 
+  // Tiles of one sequence beside each other read the same keys at about the
+  // same time, mostly from an L2 (with sequences beside each other instead,
+  // twelve ragged chunks took 508 us for 383); those that see the most tokens
+  // start first.
   uint32_t u = blockIdx.x;
   const int h = u % H;
   u /= H;
   const int part = u % a.splits;
   u /= a.splits;
-  const int tile = tiles_most - 1 - u % tiles_most;  // longest first
+  const int tile = tiles_most - 1 - u % tiles_most;
   const int s = u / tiles_most;
   const Seq sq = sequence(a.b, s);
   if (sq.rows * G <= a.split_rows_most || tile * kChunkRows >= sq.rows * G) return;
@@ -280,17 +287,25 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
     }
     if (base >= any_lim || base + kTok <= any_low) continue;
 
+    // keys are read from LDS some products ahead of their use
     f32x16 x[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < DP / 16; ++k) {
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
         const u32x4 af =
             *reinterpret_cast<const u32x4 *>(k_lds + (t * 32 + c) * KP + k * 32 + gg * 16);
         x[t] = mfma32<ACT>(af, u32x4{qreg[k][0], qreg[k][1], qreg[k][2], qreg[k][3]}, x[t]);
       }
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
     }
     auto scale_of = [&](const float *lds, const float *own, int t, int q) {
       if constexpr (TILES) {
@@ -339,11 +354,17 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
         for (int i = 0; i < 16; ++i) o[dt][i] *= fo;
       m = top;
     }
-    u32x4 pf[4];  // 16 tokens each
+    // The weights of 16 tokens are made while the products of the 16 before
+    // them run.
+    const uint8_t *vp =
+        v_lds + (gg * 4 + ((lane & 15) >> 2)) * VP + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int k = 0; k < 4; ++k) {
+      const int t = k >> 1;
+      u32x4 pf;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q2 = 0; q2 < 2; ++q2) {
+        const int q = (k & 1) * 2 + q2;
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -355,23 +376,28 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] *= f[i];
         }
-        pf[t * 2 + (q >> 1)][(q & 1) * 2] = pack_act<PV>(p[0], p[1]);
-        pf[t * 2 + (q >> 1)][(q & 1) * 2 + 1] = pack_act<PV>(p[2], p[3]);
+        pf[q2 * 2] = pack_act<PV>(p[0], p[1]);
+        pf[q2 * 2 + 1] = pack_act<PV>(p[2], p[3]);
       }
-    // lane of 16: token (lane / 4) and four elements of 16 of a transposing
-    // read; it gets one element of four tokens
-    const uint8_t *vp =
-        v_lds + (gg * 4 + ((lane & 15) >> 2)) * VP + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+      // lane of 16: token (lane / 4) and four elements of 16 of a transposing
+      // read; it gets one element of four tokens
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int dt = 0; dt < DT; ++dt) {
         const uint8_t *p = vp + k * 16 * VP + dt * 64;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * VP));
         const u32x2 x0 = __builtin_bit_cast(u32x2, lo), x1 = __builtin_bit_cast(u32x2, hi);
-        o[dt] = mfma32<PV>(u32x4{x0[0], x0[1], x1[0], x1[1]}, pf[k], o[dt]);
+        o[dt] = mfma32<PV>(u32x4{x0[0], x0[1], x1[0], x1[1]}, pf, o[dt]);
       }
+    }
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, 8, 1);
+    __builtin_amdgcn_sched_group_barrier(kValu, FP8 ? 44 : 36, 1);
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 1);
+      __builtin_amdgcn_sched_group_barrier(kValu, (FP8 ? 44 : 36) / DT, 1);
+    }
   }
 
   const float total = add_rows32(l);

@@ -215,9 +215,17 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
           ea::kArrivals * 4 + up(p.split_grid * p.heads_wg * cols * (d.head_dim + 2) * 4, 16);
   }
   if (p.chunk) {
-    const int64_t tiles = (b->max_rows * G + ea::kChunkRows - 1) / ea::kChunkRows;
-    const int64_t units = b->n_seqs * H * tiles;
-    const int64_t want = std::max<int64_t>(1, (512 + units - 1) / units);
+    // As many workgroups as the chip holds; twice as many where sequences
+    // differ, and then an odd number of parts: workgroups go to the eight XCDs
+    // in turn, heads and parts first, and shorter sequences have no last parts,
+    // so that even numbers leave XCDs without work.  Six ragged fp8 chunks of
+    // one head took 501 us in two parts, 391 in three, 508 in four; twelve of 4
+    // heads 395 in one part, 508 in two, 383 in three.
+    const int64_t most = b->n_seqs * ((b->max_rows * G + ea::kChunkRows - 1) / ea::kChunkRows);
+    const int64_t tiles = std::min(most, (int64_t)b->n_rows * G / ea::kChunkRows + b->n_seqs);
+    const int64_t target = 2LL * compute_units(ea::cache_device(c)) * (b->n_seqs > 1 ? 2 : 1);
+    int64_t want = std::max<int64_t>(1, (target + H * tiles - 1) / (H * tiles));
+    if (b->n_seqs > 1) want |= 1;
     p.chunk_tokens = (int32_t)std::max<int64_t>(up((span + want - 1) / want, ea::kChunkTokens),
                                                 512);
     // a span's start is rounded down, which can add a part of the rest
