@@ -661,8 +661,9 @@ typedef struct {
  * position p = kv_len[s] - rows + r, attends to the tokens j <= p of its
  * sequence (j > p - window; in its selected blocks), query head i to KV head
  * i / (q_heads / H).  Sums and softmax statistics are 32 bits.  A row that
- * attends to nothing gets zeros.  What lies in slots that no row of the
- * sequence attends to never matters.  workspace (16-byte aligned device
+ * attends to nothing gets zeros.  What lies in tokens that a row does not
+ * attend to never reaches it, be it infinite or NaN, and neither do scales of
+ * blocks that it has no token of.  workspace (16-byte aligned device
  * memory, ea_attend_workspace bytes; NULL when that is 0) is scratch of this
  * call: calls that may overlap need their own.  Its first 32 KiB hold
  * counters: zero when it is first used, left zero by every call, and nobody

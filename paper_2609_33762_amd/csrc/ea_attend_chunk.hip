@@ -89,7 +89,8 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   const int wg_last = min((tile * kChunkRows + kChunkRows - 1) / G, sq.rows - 1);
   int t0 = span.begin + part * a.chunk_tokens;
   const int t1 = min(min(span.end, t0 + a.chunk_tokens), pos0 + wg_last + 1);
-  if (a.window > 0) t0 = max(t0, (pos0 + wg_first + 1 - a.window) & ~(kTok - 1));
+  const int wg_low = a.window > 0 ? max(0, pos0 + wg_first + 1 - a.window) : 0;
+  t0 = max(t0, wg_low & ~(kTok - 1));
 
   uint32_t qreg[DP / 16][4];
   {
@@ -150,7 +151,8 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
           const float *sp =
               kv.scales + ((uint64_t)page[t] * (uint32_t)kv.scale_page + h * kv.scale_head);
           k_sc[t] = sp[0];
-          v_sc[t] = ok && base + t * 16 < sq.len ? sp[kv.scale_kv] : 0.f;
+          v_sc[t] = ok && base + t * 16 < sq.len && base + t * 16 + 16 > wg_low ? sp[kv.scale_kv]
+                                                                               : 0.f;
         }
       }
 #pragma unroll
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
       if (FP8) {
         const float *sp = kv.scales + (uint64_t)page * (uint32_t)kv.scale_page + h * kv.scale_head;
         k_sc[0] = ok ? sp[0] : 0.f;
-        v_sc[0] = ok ? sp[kv.scale_kv] : 0.f;
+        v_sc[0] = ok && tok >= wg_low ? sp[kv.scale_kv] : 0.f;
       }
 #pragma unroll
       for (int j = 0; j < PASS; ++j) {
@@ -235,10 +237,24 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
     load(t0);
     if (TILES) look(t0 + kTok);
   }
+  // A weight of zero does not keep out what is not finite: in tiles of which
+  // some row does not see all, such values count as zero and are left for the
+  // end.
+  const int wg_all_lim = min(pos0 + wg_first + 1, sq.len);
+  const int wg_all_low = a.window > 0 ? max(0, pos0 + wg_last + 1 - a.window) : 0;
+  uint32_t odd = 0;
   for (int base = t0; base < t1; base += kTok) {
+    const bool cut = gone || base < wg_all_low || base + kTok > wg_all_lim;
     __syncthreads();  // the last tile has been read
     float ks[TP], vs[TP];  // TILES: of 16 tokens each; else in LDS
     if (FP8) {
+      if (cut) {
+#pragma unroll
+        for (int t = 0; t < (TILES ? TP : 1); ++t) {
+          odd |= !finite(v_sc[t]);
+          v_sc[t] = finite(v_sc[t]) ? v_sc[t] : 0.f;
+        }
+      }
       float top = v_scale;
 #pragma unroll
       for (int t = 0; t < (TILES ? TP : 1); ++t) top = fmaxf(top, fabsf(v_sc[t]));
@@ -278,6 +294,19 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
       }
       *reinterpret_cast<u32x4 *>(k_lds + t * KP + chunk * 16) = x;
       *reinterpret_cast<u32x4 *>(v_lds + t * VP + chunk * 16) = y;
+    }
+    if (cut) {  // each thread's own part of the values
+      for (int j = 0; j < PASS; ++j) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(v_lds + (first_tok + j * STEP) * VP + chunk * 16);
+        u32x4 y = *p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bad = odd_mask<PV, false>(y[i]);
+          odd |= bad;
+          y[i] &= ~bad;
+        }
+        *p = y;
+      }
     }
     const uint64_t gone_here = gone;
     __syncthreads();
@@ -397,6 +426,26 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
       __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
       __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 1);
       __builtin_amdgcn_sched_group_barrier(kValu, (FP8 ? 44 : 36) / DT, 1);
+    }
+  }
+
+  if (__syncthreads_or(odd != 0)) {
+    for (int base = t0; base < t1; base += kTok) {
+      const uint32_t own = table[(uint32_t)min(over_page(kv, base + lane), last_page)];
+      if (base >= wg_all_low && base + kTok <= wg_all_lim && !__any(own >= (uint32_t)kv.num_pages))
+        continue;
+      for (int at = base; at < min(base + kTok, t1); ++at) {
+        const uint32_t page = __shfl(own, at - base), slot = at - over_page(kv, at) * T;
+        if (page >= (uint32_t)kv.num_pages) continue;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int d = dt * 32 + (i >> 2) * 8 + gg * 4 + (i & 3);
+            const float v = d < D ? odd_value<ACT, FP8>(kv, page, slot, h, d) : 0.f;
+            if (at >= low && at < lim) o[dt][i] += v;
+          }
+      }
     }
   }
 

@@ -432,6 +432,16 @@ attend_split(AttendArgs a) {
     }
   };
 
+  // whether every token of a step counts for every column
+  auto inside_of = [&](const Paged &w) {
+    if (TILES)
+      return w.tok[0] >= all_low && w.tok[1] >= all_low && w.tok[0] < all_lim - 15 &&
+             w.tok[1] < all_lim - 15;
+    return (bool)__all(w.tok[0] >= all_low && w.tok[1] >= all_low && w.tok[0] < all_lim &&
+                       w.tok[1] < all_lim);
+  };
+  uint32_t odd = 0;  // where some do not: whether a value there is not finite
+
   if (t0 < t1) {
     Paged here = checked(pages(entries(t0)));
     Paged ahead = pages(entries(t0 + kSplitStep));
@@ -473,20 +483,19 @@ attend_split(AttendArgs a) {
       }
       load_keys(next);
 
-      // position of this lane's token j; whether every token counts for every
-      // column
+      // position of this lane's token j
       auto tok = [&](int j) {
         const int t = j >> 2, r = g * 4 + (j & 3);
         if (!TILES) return __shfl(here.tok[t], r);
         return here.tok[t] == INT32_MAX ? INT32_MAX : here.tok[t] + r;
       };
-      bool inside;
-      if (TILES) {
-        inside = here.tok[0] >= all_low && here.tok[1] >= all_low &&
-                 here.tok[0] < all_lim - 15 && here.tok[1] < all_lim - 15;
-      } else {
-        inside = __all(here.tok[0] >= all_low && here.tok[1] >= all_low &&
-                       here.tok[0] < all_lim && here.tok[1] < all_lim);
+      const bool inside = inside_of(here);
+      if (FP8 && !inside) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          odd |= !finite(sc.v[j]);
+          sc.v[j] = finite(sc.v[j]) ? sc.v[j] : 0.f;
+        }
       }
       u32x4 ph[NB], pl[NB];
 #pragma unroll
@@ -531,14 +540,20 @@ attend_split(AttendArgs a) {
                                         p[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
         }
       }
-      // tokens that no column attends to: whatever lies there counts as zero
+      // A weight of zero does not keep out what is not finite: tokens that no
+      // column attends to count as zero, and of the others such values are
+      // left for the end.
       if (!inside) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int at = tok(j);
           const bool keep = at >= any_low && at < sq.len;
 #pragma unroll
-          for (int w = 0; w < VD; ++w) vb[j][w] = keep ? vb[j][w] : 0;
+          for (int w = 0; w < VD; ++w) {
+            const uint32_t v = keep ? vb[j][w] : 0, bad = odd_mask<ACT, FP8>(v);
+            odd |= bad;
+            vb[j][w] = v & ~bad;
+          }
         }
       }
 #pragma unroll
@@ -572,6 +587,34 @@ attend_split(AttendArgs a) {
       load_values(next);
       here = next;
       sc = sc_next;
+    }
+  }
+
+  // ---- values that are not finite, where not every column attends to them
+  if (__any(odd != 0)) {
+    for (int base = t0; base < t1; base += kSplitStep) {
+      const Paged w = checked(pages(entries(base)));
+      if (inside_of(w)) continue;
+      for (int j = 0; j < kSplitStep; ++j) {
+        const int t = j >> 4, r = j & 15;
+        const uint32_t page_of = t ? w.page[1] : w.page[0], slot_of = t ? w.slot[1] : w.slot[0];
+        int at = t ? w.tok[1] : w.tok[0];
+        const uint32_t page = TILES ? page_of : __shfl(page_of, r);
+        const uint32_t slot = TILES ? slot_of + r : __shfl(slot_of, r);
+        if (!TILES) at = __shfl(at, r);
+        if (at == INT32_MAX) continue;
+        if (TILES) at += r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const int d = (g * 4 + i) * VE + e;
+            const float v = d < D ? odd_value<ACT, FP8>(kv, page, slot, h, d) : 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              if (at >= low[nb] && at < lim[nb]) o[nb][e][i] += v;
+          }
+      }
     }
   }
 

@@ -189,6 +189,44 @@ __device__ inline uint32_t fp8_pair(uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
+// Ones in place of those of a word's two 16-bit values or four fp8 codes that
+// are not finite: a one added at the exponent's end (fp8: at the code's end,
+// only NaN has all ones) carries into the sign's place.
+template <int ACT, bool FP8>
+__device__ inline uint32_t odd_mask(uint32_t w) {
+  if constexpr (FP8) {
+    const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return (t - (t >> 7)) | t;
+  } else {
+    const uint32_t t = ((w & 0x7fff7fffu) + (ACT == kBf16 ? 0x00800080u : 0x04000400u)) &
+                       0x80008000u;
+    return (t - (t >> 15)) | t;
+  }
+}
+
+// What the value of token `slot` of a page adds to a sum where it, or its
+// scale, is not finite; zero where both are.
+template <int ACT, bool FP8>
+__device__ inline float odd_value(const KvLayer &kv, uint32_t page, uint32_t slot, int h, int d) {
+  const uint64_t at = ((uint64_t)slot * kv.heads + h) * kv.head_dim + d;
+  const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece + (uint32_t)kv.piece / 2);
+  float v;
+  if constexpr (FP8) {
+    const float scale = kv.scales[(uint64_t)page * (uint32_t)kv.scale_page + h * kv.scale_head +
+                                  kv.scale_kv];
+    const uint32_t code = p[at] & 0x7f;
+    v = finite(scale) ? 0.f : scale;
+    if (code == 0x7f || (code == 0 && !finite(scale))) v = __uint_as_float(0x7fc00000u);
+    if (p[at] & 0x80) v = -v;
+  } else {
+    const uint32_t w = reinterpret_cast<const uint16_t *>(p)[at];
+    const uint32_t fraction = w & (ACT == kBf16 ? 0x7fu : 0x3ffu);
+    v = __uint_as_float((w & 0x8000u) << 16 | 0x7f800000u | (fraction ? 0x400000u : 0));
+    if (!odd_mask<ACT, false>(w)) v = 0.f;
+  }
+  return v;
+}
+
 template <int ACT>
 __device__ inline f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
   if constexpr (ACT == kBf16)
