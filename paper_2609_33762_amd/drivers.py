@@ -1,5 +1,6 @@
-"""Workload drivers over the C ABI: the agent pool, dense scattered batches
-and the layer-pipelined prefix load.  Each driver only issues library calls
+"""Workload drivers over the C ABI: the agent pool, turns that serve a layered
+model from the cache, dense scattered batches and the layer-pipelined prefix
+load.  Each driver only issues library calls
 (hash, lookup, admission, alloc, store, load, unpin) and records what it did,
 so that the tests can replay every call on the oracle and the benchmark can
 time them.  Page contents of the agent pool are a counter-based function of
@@ -218,6 +219,119 @@ class AgentPool:
         self.turn_no += 1
         return TurnRecord(t, a, len(prompt), keys, h, hit_slots, save, mask, slots,
                           int(ok.sum()), loaded_ok, load_pages, store_pages)
+
+
+# ------------------------------------------------------------ served turns
+
+class ServedTurns:
+    """Turns of one agent at a time on a layered model whose KV lives in
+    `cache`: a turn restores the prefix that the tier holds, a layer ahead of
+    its use, appends and attends to the rest of the prompt as one chunk, then
+    makes new tokens one by one, each KV head attending to `budget` blocks
+    that it selects, and stores the blocks it filled.
+
+    The model is the caller's: embed(tokens) -> x [n, ..], project(layer, x)
+    -> q, k, v [n, heads, D], mix(layer, x, attention) -> x, next(x) -> the
+    token after the last row, all on the current stream.  An fp8 cache's
+    head_scales travel beside the blocks: scale_cache describes the plane as
+    a cache (page_tokens 1, head_dim 1, elem_bytes 4) and scale_tier is its
+    tier.  Bounds are made again from the restored keys."""
+
+    def __init__(self, torch, cache, tier, model, budget, rope=None, scale_cache=None,
+                 scale_tier=None, max_tokens=65536):
+        if tier.chunk_pages != 1 or (scale_tier is not None and scale_tier.chunk_pages != 1):
+            raise ValueError("served turns keep one page in a slot")
+        if (cache.head_scales is None) != (scale_cache is None):
+            raise ValueError("head_scales need a scale_cache and a scale_tier, and only they do")
+        self.torch, self.cache, self.model, self.budget, self.rope = torch, cache, model, budget, rope
+        self.pairs = [(tier, cache)]  # last: the blocks, whose events say a layer is there
+        if scale_cache is not None:
+            self.pairs.insert(0, (scale_tier, scale_cache))
+        self.device, self.T = cache.kv.device, cache.page_tokens
+        self.max_tokens = max_tokens
+        self.copy_stream = torch.cuda.Stream(self.device)
+
+    def _ints(self, values):
+        return self.torch.as_tensor(np.ascontiguousarray(values, np.int32), device=self.device)
+
+    def _restore(self, keys, pages):
+        """Blocks of the prefix on their way, (count, an event a layer)."""
+        found = [t.lookup(keys) for t, _ in self.pairs]
+        n = min(h for h, _ in found)
+        self.copy_stream.wait_stream(self.torch.cuda.current_stream(self.device))
+        for (tier, cache), (_, slots) in zip(self.pairs, found):
+            events = [self.torch.cuda.Event() for _ in range(cache.num_layers)]
+            if n:
+                tier.load_layered(cache, slots[:n], pages[:n], self.copy_stream, events)
+            if len(slots):
+                tier.unpin(slots)  # the library orders later stores after these loads
+        return n, events
+
+    def _store(self, keys, pages):
+        """The blocks that the tier does not hold yet; how many went."""
+        for tier, cache in self.pairs:
+            _, slots = tier.alloc(keys)
+            new = slots >= 0
+            if new.any():
+                tier.store(cache, pages[new], slots[new])
+                tier.unpin(slots[new])
+        return int(new.sum())
+
+    def turn(self, prompt, n_new, pages):
+        """prompt: int32 tokens; pages: pages for the prompt and n_new tokens,
+        the caller's, free of any transfer.  Returns the tokens made, the
+        blocks restored and the blocks stored."""
+        torch, cache, model, T = self.torch, self.cache, self.model, self.T
+        prompt, pages = np.asarray(prompt, np.int32), np.asarray(pages, np.int32)
+        n = len(prompt)
+        if not 1 <= n or n_new < 0 or n + n_new > min(self.max_tokens, len(pages) * T):
+            raise ValueError("the turn's tokens do not fit its pages")
+        keys, _ = api.hash_blocks(prompt, np.array([0, n]), T)
+        full = (n - 1) // T  # blocks that may come from the tier: a row is left to compute
+        held, events = self._restore(keys[:full], pages)
+        table, start = self._ints(pages[None]), held * T
+        restored = self._ints(pages[:held])
+
+        # the rest of the prompt, one chunk
+        rows = n - start
+        batch = api.Batch(table, self._ints([n]), n, self._ints([0, rows]), rows, rows)
+        x = model.embed(torch.as_tensor(prompt[start:], device=self.device))
+        for layer in range(cache.num_layers):
+            if held:
+                torch.cuda.current_stream(self.device).wait_event(events[layer])
+                if cache.bounds is not None:
+                    cache.bound_blocks(restored, layer, 1, dtype=x.dtype)
+            x = self._layer(layer, batch, x)
+
+        # new tokens, one by one; the last one made is not in the cache
+        length, made = self._ints([n]), []
+        batch = api.Batch(table, length, n + n_new)
+        chosen = torch.empty((1, cache.num_kv_heads, self.budget), dtype=torch.int32,
+                             device=self.device)
+        for i in range(n_new):
+            made.append(model.next(x))
+            if i == n_new - 1:
+                break
+            length.add_(1)
+            x = model.embed(torch.as_tensor(made[-1:], dtype=torch.int32, device=self.device))
+            for layer in range(cache.num_layers):
+                x = self._layer(layer, batch, x, chosen)
+
+        in_cache = np.concatenate([prompt, np.asarray(made[:-1], np.int32)])
+        keys, _ = api.hash_blocks(in_cache, np.array([0, len(in_cache)]), T)
+        stored = self._store(keys[held:], pages[held:len(keys)]) if len(keys) > held else 0
+        return made, held, stored
+
+    def _layer(self, layer, batch, x, chosen=None):
+        cache = self.cache
+        q, k, v = self.model.project(layer, x)
+        turned = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        cache.append_kv(layer, batch, k, v, rope=self.rope, q=q, q_out=turned)
+        if chosen is not None:
+            cache.select_blocks(layer, batch, turned, chosen)
+        out = self.torch.empty_like(turned)
+        cache.attend(layer, batch, turned, out, selected=chosen)
+        return self.model.mix(layer, x, out)
 
 
 # ------------------------------------------------- dense scattered batches
