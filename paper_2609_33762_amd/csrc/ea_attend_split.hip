@@ -26,6 +26,11 @@
 // Matrix units idle for most of the time, which pays for P as a sum of two
 // bf16 (16 bits of it) beside bf16 or fp8 values; with f16 values P is one
 // f16 (11 bits) held at up to 2^15, so that small weights keep their bits.
+//
+// Measured: 64 sequences of 8,192-65,536 fp8 tokens, one KV head of 8, 623 MB
+// in 117 us (5.3 TB/s; reading random pages alone reaches 6.0); one sequence
+// of 4 KV heads and 65,536 16-bit tokens, 134 MB, in 33 us, of which some 10
+// are the launch, the first loads' latency and the join.
 #include <hip/hip_runtime.h>
 
 #include "ea_kv_device.hpp"
@@ -131,8 +136,8 @@ __device__ inline void join_parts(const AttendArgs &a, int w0, int stride, int p
 
 // The work of a call in steps of 32 tokens for each run of a workgroup: a
 // sequence has `units` units (heads_wg KV heads; with selections, a row and
-// its KV head) of `steps` steps each.  Every wave of every workgroup finds the same totals from the
-// sequences' lengths, which only the device knows.
+// its KV head) of `steps` steps each.  Every wave of every workgroup finds the
+// same totals from the sequences' lengths, which only the device knows.
 struct SeqWork {
   Seq q;
   int32_t units, steps;
@@ -710,7 +715,8 @@ attend_split(AttendArgs a) {
 constexpr int kJoinWaves = 4;
 
 // Join of the chunk kernel's parts: one wave a row and head, a lane four
-// elements.
+// elements.  It reads the parts once, a launch of its own after the products
+// (a few us of hundreds).
 template <int ACT>
 __global__ __launch_bounds__(kJoinWaves *kLanes) void attend_join(AttendArgs a) {
   const int HQ = a.kv.heads * a.group, D = a.kv.head_dim;
