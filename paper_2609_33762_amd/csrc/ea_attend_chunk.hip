@@ -16,7 +16,7 @@
 // maximum hold.
 //
 // Measured: 2,048 rows of 4 KV heads of 8 over 26,624 16-bit tokens, 0.86
-// TFLOP, in 0.95 ms (0.91 PFLOP/s; a large library product reaches 1.3), ragged
+// TFLOP, in 0.93 ms (0.93 PFLOP/s; a large library product reaches 1.3), ragged
 // fp8 chunks of 0.22 TFLOP in 0.42 ms.  Per tile the softmax takes about as
 // many cycles of a SIMD as the products, and two waves a SIMD hide it in part.
 #include <hip/hip_runtime.h>
