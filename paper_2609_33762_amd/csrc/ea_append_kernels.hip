@@ -239,7 +239,8 @@ __device__ inline void append_block(const AppendArgs &a, uint32_t u, int lane) {
   auto fetch = [&](int t, float x[16]) {
     Angles an = {};
     if (rope) an = angles_of(rope, p * T + t, a.rope_dim, at);
-    rotated<ACT, HALVES>(head + t * src.row_stride, at, rope, p * T + t, a.rope_dim, a.interleaved, an, x);
+    rotated<ACT, HALVES>(head + t * src.row_stride, at, rope, p * T + t, a.rope_dim,
+                         a.interleaved, an, x);
   };
   // the first passes' tokens; a block of more is read again below
   float x[KEEP][16];
@@ -378,7 +379,8 @@ __device__ inline void rotate_queries(const AppendArgs &a, uint32_t u, int lane)
     const int h = h0 + i + lane / LP;
     if (h >= a.q_heads) break;
     float x[16];
-    rotated<ACT, HALVES>(src + h * a.q.head_stride, at, a.rope, pos, a.rope_dim, a.interleaved, an, x);
+    rotated<ACT, HALVES>(src + h * a.q.head_stride, at, a.rope, pos, a.rope_dim, a.interleaved,
+                         an, x);
 #pragma unroll
     for (int n = 0; n < 2; ++n)
       if (at.in[n])

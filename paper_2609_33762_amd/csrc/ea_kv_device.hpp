@@ -170,10 +170,6 @@ __device__ inline float act_to_float(uint16_t v) {
   return (float)__builtin_bit_cast(typename ActOf<ACT>::T, v);
 }
 template <int ACT>
-__device__ inline uint16_t float_to_act(float v) {
-  return __builtin_bit_cast(uint16_t, (typename ActOf<ACT>::T)v);
-}
-template <int ACT>
 __device__ inline uint32_t pack_act(float lo, float hi) {
   typedef typename ActOf<ACT>::T V2 __attribute__((ext_vector_type(2)));
   const V2 v = {(typename ActOf<ACT>::T)lo, (typename ActOf<ACT>::T)hi};  // one instruction

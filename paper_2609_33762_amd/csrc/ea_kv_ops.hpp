@@ -64,9 +64,10 @@ struct AttendArgs {
   // Sequences with at most this many rows times heads of a group go to the
   // split kernel, others to the chunk kernel.
   int32_t split_rows_most;
-  // Split kernel: a workgroup takes heads_wg (1 or 2) neighbouring KV heads.  A unit (a sequence and as many heads) is split so that
-  // the parts of all fit split_wgs workgroups where they can, a part having
-  // least_steps steps at least; split_grid workgroups are enough for that.
+  // Split kernel: a workgroup takes heads_wg (1 or 2) neighbouring KV heads.
+  // A unit (a sequence and as many heads) is split so that the parts of all
+  // fit split_wgs workgroups where they can, a part having least_steps steps
+  // at least; split_grid workgroups are enough for that.
   // Their parts, and the counts of a unit's parts done, zero between calls.
   int32_t heads_wg, split_wgs, least_steps, split_grid;
   float *split_parts;

@@ -243,7 +243,8 @@ class ServedTurns:
             raise ValueError("served turns keep one page in a slot")
         if (cache.head_scales is None) != (scale_cache is None):
             raise ValueError("head_scales need a scale_cache and a scale_tier, and only they do")
-        self.torch, self.cache, self.model, self.budget, self.rope = torch, cache, model, budget, rope
+        self.torch, self.cache, self.model = torch, cache, model
+        self.budget, self.rope = budget, rope
         self.pairs = [(tier, cache)]  # last: the blocks, whose events say a layer is there
         if scale_cache is not None:
             self.pairs.insert(0, (scale_tier, scale_cache))
@@ -259,12 +260,15 @@ class ServedTurns:
         found = [t.lookup(keys) for t, _ in self.pairs]
         n = min(h for h, _ in found)
         self.copy_stream.wait_stream(self.torch.cuda.current_stream(self.device))
-        for (tier, cache), (_, slots) in zip(self.pairs, found):
-            events = [self.torch.cuda.Event() for _ in range(cache.num_layers)]
-            if n:
-                tier.load_layered(cache, slots[:n], pages[:n], self.copy_stream, events)
-            if len(slots):
-                tier.unpin(slots)  # the library orders later stores after these loads
+        try:
+            for (tier, cache), (_, slots) in zip(self.pairs, found):
+                events = [self.torch.cuda.Event() for _ in range(cache.num_layers)]
+                if n:
+                    tier.load_layered(cache, slots[:n], pages[:n], self.copy_stream, events)
+        finally:  # the library orders later stores after these loads
+            for (tier, _), (_, slots) in zip(self.pairs, found):
+                if len(slots):
+                    tier.unpin(slots)
         return n, events
 
     def _store(self, keys, pages):
@@ -273,8 +277,10 @@ class ServedTurns:
             _, slots = tier.alloc(keys)
             new = slots >= 0
             if new.any():
-                tier.store(cache, pages[new], slots[new])
-                tier.unpin(slots[new])
+                try:
+                    tier.store(cache, pages[new], slots[new])
+                finally:
+                    tier.unpin(slots[new])
         return int(new.sum())
 
     def turn(self, prompt, n_new, pages):
