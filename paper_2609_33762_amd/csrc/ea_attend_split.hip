@@ -189,10 +189,10 @@ attend_split(AttendArgs a) {
     all += w.units * w.steps;
   }
   all = __builtin_amdgcn_readlane(scan_wave(all), kLanes - 1);
-  int each = max((all + a.split_wgs - 1) / a.split_wgs, a.least_steps);
-  for (int i = 0; a.b.n_seqs <= kLanes; ++i) {
-    const int n = __builtin_amdgcn_readlane(scan_wave(sw.units * ((sw.steps + each - 1) / each)),
-                                            kLanes - 1);
+  int each = a.least_steps ? max(parts_of_steps(all, a.split_wgs), a.least_steps) : INT32_MAX;
+  for (int i = 0; a.least_steps && a.b.n_seqs <= kLanes; ++i) {
+    const int n = __builtin_amdgcn_readlane(
+        scan_wave(sw.units * parts_of_steps(sw.steps, each)), kLanes - 1);
     if (n <= a.split_wgs || i == 3) break;
     each = each + max(1, (int)((float)each * (n - a.split_wgs) / a.split_wgs));
   }
@@ -201,7 +201,7 @@ attend_split(AttendArgs a) {
   int steps = 0;
   for (int s0 = 0; s0 < a.b.n_seqs; s0 += kLanes) {
     if (s0) sw = work_of<W>(a, s0 + lane);
-    const int in = (sw.steps + each - 1) / each;
+    const int in = parts_of_steps(sw.steps, each);
     const int upto = scan_wave(sw.units * in);
     const uint64_t found = __ballot(unit < upto);
     if (found) {

@@ -207,8 +207,9 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
     p.split_wgs = std::min(compute_units(ea::cache_device(c)) *
                                ea::split_resident(d.head_dim, (int32_t)cols),
                            ea::kArrivals - ea::kSplitUnits);
-    p.least_steps = units <= ea::kSplitUnits ? 2 : INT32_MAX;
-    const int64_t whole = (steps + p.least_steps - 1) / p.least_steps;  // most parts of a unit
+    p.least_steps = units <= ea::kSplitUnits ? 2 : 0;
+    // most parts of a unit
+    const int64_t whole = p.least_steps ? (steps + p.least_steps - 1) / p.least_steps : 1;
     p.split_grid = (int32_t)std::min<int64_t>(p.split_wgs + units, units * whole);
     if (p.split_grid > units)
       p.split_bytes =

@@ -67,7 +67,8 @@ struct AttendArgs {
   // Split kernel: a workgroup takes heads_wg (1 or 2) neighbouring KV heads.
   // A unit (a sequence and as many heads) is split so that the parts of all
   // fit split_wgs workgroups where they can, a part having least_steps steps
-  // at least; split_grid workgroups are enough for that.
+  // at least (0: units are not split); split_grid workgroups are enough for
+  // that.
   // Their parts, and the counts of a unit's parts done, zero between calls.
   int32_t heads_wg, split_wgs, least_steps, split_grid;
   float *split_parts;
@@ -91,6 +92,13 @@ struct SelectArgs {
   int32_t blocks_wave;      // blocks one wave scores
 };
 
+// Parts of at most `each` steps that `steps` steps come in.  No sum of the two,
+// which could pass 32 bits.
+constexpr int32_t parts_of_steps(int32_t steps, int32_t each) {
+  return steps > 0 ? (steps - 1) / each + 1 : 0;
+}
+static_assert(parts_of_steps(0, INT32_MAX) == 0 && parts_of_steps(INT32_MAX, INT32_MAX) == 1 &&
+              parts_of_steps(INT32_MAX, 1) == INT32_MAX && parts_of_steps(5, 2) == 3);
 
 // Columns of the split kernel's variant for this many; waves of a variant's
 // workgroups, and the workgroups of it that its registers let a compute unit

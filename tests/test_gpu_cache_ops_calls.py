@@ -1,0 +1,135 @@
+"""The cache operators call by call: calls of many units, calls that share a
+workspace, captured calls, steps whose rows only the device knows, selections
+in any order.  Compared with 64-bit computations; the bounds of the errors are
+those of tests/test_gpu_cache_ops.py."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_cache_ops as base
+from gpu_common import need_gpu
+from paper_2609_33762_amd import api
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, FP8 = base.BF16, base.F16, base.FP8
+FEW, MANY = 2.0 ** -15, 2.0 ** -8  # rounding of bf16 kernels' weights: few rows, a chunk's
+
+
+class Step:
+    """Sequences over one small cache of random pages, which they share."""
+
+    def __init__(self, lens, rows, heads, group, dim, page=16, pages=96, seed=0, max_kv=None,
+                 n_rows=None, max_rows=None):
+        need_gpu()
+        self.g = torch.Generator().manual_seed(seed)
+        self.H, self.G, self.D, self.T = heads, group, dim, page
+        self.lens, self.rows = list(lens), list(rows)
+        self.starts = [0]
+        for n in self.rows:
+            self.starts.append(self.starts[-1] + n)
+        self.n_rows = self.starts[-1] if n_rows is None else n_rows
+        self.kv = torch.randn((1, pages, 2, page, heads, dim), generator=self.g).to(BF16).cuda()
+        self.max_kv = max(self.lens + [1]) if max_kv is None else max_kv
+        self.table = torch.randint(pages, (len(self.lens), -(-self.max_kv // page)),
+                                   generator=self.g, dtype=torch.int32).cuda()
+        self.cache = api.Cache(self.kv, pages, 1, page, heads, dim, 2)
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.kv_len, self.row_start = ints(self.lens), ints(self.starts)
+        self.max_rows = max(self.rows + [1]) if max_rows is None else max_rows
+        self.batch = self.new_batch()
+        self.q = torch.randn((self.n_rows, heads * group, dim), generator=self.g).to(BF16).cuda()
+
+    def new_batch(self):
+        return api.Batch(self.table, self.kv_len, self.max_kv, self.row_start, self.n_rows,
+                         self.max_rows)
+
+    def choose(self, budget):
+        """Distinct random blocks for every row and head, among the blocks up
+        to its sequence's last one, -1 after them."""
+        sel = torch.full((self.n_rows, self.H, budget), -1, dtype=torch.int32)
+        for s, n in enumerate(self.rows):
+            held = -(-self.lens[s] // self.T)
+            take = min(held, budget)
+            some = torch.rand((n, self.H, held), generator=self.g).argsort(-1)[..., :take]
+            sel[self.starts[s]:self.starts[s + 1], :, :take] = some.sort(-1).values.int()
+        return sel.cuda()
+
+    def exact(self, selected=None):
+        """(output, sum of weights times |v|, log-sum-exp) in 64 bits."""
+        H, G, D, T = self.H, self.G, self.D, self.T
+        kv = self.kv[0].double()
+        o = torch.zeros((self.n_rows, H * G, D), dtype=torch.float64, device="cuda")
+        a, lse = torch.zeros_like(o), torch.full((self.n_rows, H * G), -math.inf,
+                                                 dtype=torch.float64, device="cuda")
+        for s, n in enumerate(self.rows):
+            length, at = self.lens[s], self.starts[s]
+            if n == 0 or length == 0:
+                continue
+            pages = self.table[s, :-(-length // T)].long()
+            k, v = (kv[pages, i].reshape(-1, H, D)[:length].transpose(0, 1).contiguous()
+                    for i in (0, 1))
+            tok = torch.arange(length, device="cuda")
+            see = tok <= length - n + torch.arange(n, device="cuda")[:, None]
+            see = see.expand(H, n, length)
+            if selected is not None:
+                ids = selected[at:at + n].transpose(0, 1).long()  # [H, n, budget]
+                ok = (ids >= 0) & (ids < len(pages))
+                held = torch.zeros((H, n, len(pages) + 1), dtype=torch.bool, device="cuda")
+                held.scatter_(2, torch.where(ok, ids, len(pages)), True)
+                see = see & held[:, :, tok // T]
+            q = self.q[at:at + n].double().view(n, H, G, D).permute(1, 0, 2, 3)
+            x = torch.matmul(q.reshape(H, n * G, D), k.transpose(1, 2).contiguous())
+            x = x.view(H, n, G, length) * D ** -0.5
+            x = x.masked_fill(~see[:, :, None], -math.inf)
+            w = torch.softmax(x, -1).nan_to_num(0.0).view(H, n * G, length)
+            for y, u in ((o, v), (a, v.abs())):
+                y[at:at + n] = torch.matmul(w, u).view(H, n, G, D).permute(1, 0, 2, 3).reshape(
+                    n, H * G, D)
+            lse[at:at + n] = torch.logsumexp(x, -1).permute(1, 0, 2).reshape(n, H * G)
+        return o, a, lse
+
+    def attend(self, batch=None, **kw):
+        out = torch.full_like(self.q, math.nan)
+        lse = torch.full((self.n_rows, self.H * self.G), math.nan, device="cuda")
+        self.cache.attend(0, self.batch if batch is None else batch, self.q, out, lse=lse, **kw)
+        return out, lse
+
+    def check(self, got, weights, selected=None, rows=slice(None)):
+        o, a, want = self.exact(selected)
+        o, a, want = o[rows], a[rows], want[rows]
+        out, lse = got[0][rows].double(), got[1][rows].double()
+        assert torch.isfinite(out).all()
+        bound = base.ULP[BF16] * o.abs() + (weights + 2.0 ** -14) * a + 2.0 ** -25
+        assert ((out - o).abs() <= bound).all()
+        empty = torch.isinf(want)
+        assert torch.equal(empty, lse == -math.inf)
+        assert ((lse - want)[~empty].abs() < 1e-4 * (1 + want[~empty].abs())).all()
+
+
+# ---------------------------------------------------------- many units of work
+
+def spread(lo, hi, n):
+    return [lo + (i * 37) % (hi - lo + 1) for i in range(n)]
+
+
+@pytest.mark.parametrize("n,heads,group,hi", [(4200, 1, 2, 700), (1100, 8, 1, 400), (530, 8, 2, 900)])
+def test_more_sequences_and_heads_than_are_split(n, heads, group, hi):
+    # a unit is a sequence and one or two heads; several steps each
+    st = Step(spread(1, hi, n), [1] * n, heads, group, 64)
+    st.check(st.attend(), FEW)
+
+
+@pytest.mark.parametrize("n,rows,heads,budget,hi", [
+    (1, 1100, 4, 20, 1500),   # one sequence, several steps
+    (1, 4200, 1, 4, 4200),    # one step each
+    (40, 30, 4, 20, 600),
+    (600, 3, 4, 20, 400),     # more sequences than lanes, and ragged rows
+])
+def test_more_selected_rows_and_heads_than_are_split(n, rows, heads, budget, hi):
+    rows = [rows] * n if n < 600 else [1 + i % rows for i in range(n)]
+    lens = [max(a, r) for a, r in zip(spread(hi // 2, hi, n), rows)]
+    st = Step(lens, rows, heads, 2, 64)
+    sel = st.choose(budget)
+    st.check(st.attend(selected=sel), FEW, selected=sel)
