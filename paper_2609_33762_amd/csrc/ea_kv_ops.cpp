@@ -162,12 +162,13 @@ int compute_units(int dev) {
 }
 
 // How an attention call is split along its tokens, and its workspace: the
-// counters, the split kernel's parts, the chunk kernel's parts.
+// counters, always first, the split kernel's parts, the chunk kernel's parts.
+constexpr int64_t kCounters = ea::kArrivals * 4;
 struct Parts {
   bool split, chunk;  // kernels to launch
   int32_t heads_wg, split_wgs, least_steps, split_grid;
   int32_t splits, chunk_tokens;
-  int64_t split_bytes, chunk_bytes, bytes;  // the first with the counters
+  int64_t split_bytes, chunk_bytes, bytes;  // the last with the counters
 };
 
 Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
@@ -212,8 +213,7 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
     const int64_t whole = p.least_steps ? (steps + p.least_steps - 1) / p.least_steps : 1;
     p.split_grid = (int32_t)std::min<int64_t>(p.split_wgs + units, units * whole);
     if (p.split_grid > units)
-      p.split_bytes =
-          ea::kArrivals * 4 + up(p.split_grid * p.heads_wg * cols * (d.head_dim + 2) * 4, 16);
+      p.split_bytes = up(p.split_grid * p.heads_wg * cols * (d.head_dim + 2) * 4, 16);
   }
   if (p.chunk) {
     // As many workgroups as the chip holds; twice as many where sequences
@@ -236,7 +236,8 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
       p.chunk_bytes =
           up((int64_t)b->n_rows * a->q_heads * p.splits * (d.head_dim + 2) * 4, 16);
   }
-  p.bytes = p.split_bytes + p.chunk_bytes;
+  // whichever kernels run, so that calls of other shapes find the counters zero
+  if (p.split_bytes + p.chunk_bytes > 0) p.bytes = kCounters + p.split_bytes + p.chunk_bytes;
   return p;
 }
 
@@ -393,10 +394,10 @@ int ea_attend(ea_cache *c, const ea_cache_planes *planes, int32_t layer, const e
   k.heads_wg = p.heads_wg;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   k.arrivals = reinterpret_cast<int32_t *>(ws);
-  k.split_parts = reinterpret_cast<float *>(ws + ea::kArrivals * 4);
+  k.split_parts = reinterpret_cast<float *>(ws + kCounters);
   k.splits = p.splits;
   k.chunk_tokens = p.chunk_tokens;
-  k.part_o = reinterpret_cast<float *>(ws + p.split_bytes);
+  k.part_o = reinterpret_cast<float *>(ws + kCounters + p.split_bytes);
   k.part_ml = k.part_o + (int64_t)b->n_rows * a->q_heads * p.splits * d.head_dim;
   const int fp8 = d.elem_bytes == 1;
   OnDevice on(ea::cache_device(c));

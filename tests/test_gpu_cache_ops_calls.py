@@ -2,6 +2,7 @@
 workspace, captured calls, steps whose rows only the device knows, selections
 in any order.  Compared with 64-bit computations; the bounds of the errors are
 those of tests/test_gpu_cache_ops.py."""
+import ctypes as C
 import math
 
 import pytest
@@ -9,6 +10,7 @@ import torch
 
 import test_gpu_cache_ops as base
 from gpu_common import need_gpu
+from paper_2609_33762_amd import _native as N
 from paper_2609_33762_amd import api
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +135,59 @@ def test_more_selected_rows_and_heads_than_are_split(n, rows, heads, budget, hi)
     st = Step(lens, rows, heads, 2, 64)
     sel = st.choose(budget)
     st.check(st.attend(selected=sel), FEW, selected=sel)
+
+
+# ------------------------------------------------- calls that share a workspace
+
+COUNTERS = 32 << 10  # bytes at a workspace's start that every call leaves zero
+
+
+class OneWorkspace:
+    """The C entry point on a workspace of the caller's."""
+
+    def __init__(self, nbytes):
+        self.memory = torch.full((nbytes,), 0x55, dtype=torch.uint8, device="cuda")
+        self.memory[:COUNTERS] = 0
+
+    def attend(self, st, window=0, selected=None):
+        lib, ref = N.load(), C.byref
+        out = torch.full_like(st.q, math.nan)
+        lse = torch.full((st.n_rows, st.H * st.G), math.nan, device="cuda")
+        rows = [N.Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (st.q, out)]
+        a = N.Attention(*rows, lse.data_ptr(), None if selected is None else selected.data_ptr(),
+                        0 if selected is None else selected.shape[2], window, st.H * st.G, N.EA_BF16,
+                        st.D ** -0.5, 0)
+        b = st.batch.ref
+        need = lib.ea_attend_workspace(st.cache.handle, b, ref(a))
+        assert 0 <= need <= self.memory.numel()
+        planes = N.CachePlanes(None, None, None)
+        N.check("ea_attend", lib.ea_attend(st.cache.handle, ref(planes), 0, b, ref(a),
+                                           self.memory.data_ptr() if need else None, need,
+                                           api.current_stream()))
+        torch.cuda.synchronize()
+        assert not self.memory[:COUNTERS].any(), "counters are left zero by every call"
+        return (out, lse), need
+
+
+def test_chunks_decodes_and_selections_share_a_workspace():
+    chunk = Step([6000], [40], 1, 4, 64)                 # the chunk kernel alone, in parts
+    ragged = Step([3000, 2500, 40], [40, 1, 2], 1, 4, 64)  # both kernels
+    decode = Step([5000, 333], [1, 1], 1, 4, 64)         # the split kernel alone, in parts
+    sel = chunk.choose(40)
+    ws = OneWorkspace(64 << 20)
+    for order in ("cdsr", "rscd", "dcrs"):
+        for what in order:
+            st = {"c": chunk, "s": chunk, "d": decode, "r": ragged}[what]
+            got, need = ws.attend(st, selected=sel if what == "s" else None)
+            assert need > COUNTERS  # parts, or this shows nothing
+            st.check(got, FEW if what in "ds" else MANY, selected=sel if what == "s" else None)
+
+
+def test_a_batch_s_calls_of_two_shapes():
+    # one batch, one stream: dense in the chunk kernel's parts, then the selection in the
+    # split kernel's
+    st = Step([9000], [100], 1, 8, 128)
+    sel = st.choose(64)
+    for _ in range(2):
+        st.check(st.attend(), MANY)
+        st.check(st.attend(selected=sel), FEW, selected=sel)
