@@ -647,7 +647,8 @@ typedef struct {
                               the sum of exponentials, -inf for an empty row  */
   const int32_t *selected; /* int32 [n_rows][H][budget] or NULL: the blocks
                               (positions in the page table) a row's KV head
-                              attends to; others, as -1, are skipped          */
+                              attends to, each once, in any order and place;
+                              others, as -1, are skipped                      */
   int32_t budget;
   int32_t window;          /* > 0: only the last `window` tokens up to a row's
                               own; 0: all.  Must be 0 with `selected`         */

@@ -221,10 +221,6 @@ attend_split(AttendArgs a) {
   const int part = unit % parts, h0 = unit / parts % HG * HW, row_of = unit / parts / HG;
   // the wave's head, and its run of the part's tokens
   const int hw = wave % HW, h = h0 + hw, runs = W / HW, my_run = wave / HW;
-  const int share = steps / parts, more_for = steps % parts;
-  const int from = part * share + min(part, more_for);  // its steps
-  const int to = from + share + (part < more_for ? 1 : 0);
-
   const int first_pos = sq.len - sq.rows;  // of the sequence's first row
   int row0 = sq.row0, rows = sq.rows;
   const int32_t *sel = nullptr;
@@ -234,9 +230,20 @@ attend_split(AttendArgs a) {
     sel = a.selected + ((int64_t)row0 * H + h) * a.budget;
   }
   const int pos0 = first_pos + row_of;  // position of the first row
-  const Span span = span_of(a, sq, pos0);
-  // this part's tokens, and the wave's of them
-  const int step = runs * kSplitStep, run = (to - from) * kSplitStep;
+  Span span = span_of(a, sq, pos0);
+  const int step = runs * kSplitStep;
+  if (sel && pos0 >= 0 && span.end < a.budget * T) {
+    // skipped places may come before blocks.  Looked for only where there are
+    // more places than blocks: 64 contexts of 300 tokens with 128 places 10.6
+    // -> 11.4 us; walking every place instead 23.9
+    span.end = listed_of(sel, a.budget, over_page(kv, pos0)) * T;
+    steps = (span.end + step - 1) / step;
+  }
+  // this part's steps and tokens, and the wave's of them
+  const int share = steps / parts, more_for = steps % parts;
+  const int from = part * share + min(part, more_for);
+  const int to = from + share + (part < more_for ? 1 : 0);
+  const int run = (to - from) * kSplitStep;
   const int p0 = span.begin + from * step, p1 = min(span.end, span.begin + to * step);
   const int t0 = p0 + my_run * run, t1 = min(p1, t0 + run);
   const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;

@@ -67,7 +67,9 @@ __device__ inline int32_t sequence_of_row(const BatchRows &b, int32_t row) {
 
 // The tokens [begin, end) that any row of a sequence attends to, counted
 // along the selection where there is one, and the parts the chunk kernel
-// splits them into.
+// splits them into.  Of a selection with more places than the row has blocks
+// `end` is what its blocks fill where they come first; listed_of says where
+// they end.
 struct Span {
   int32_t begin, end, parts;
 };
@@ -83,6 +85,26 @@ __device__ inline Span span_of(const AttendArgs &a, const Seq &q, int32_t pos) {
   }
   s.parts = max(1, (s.end - s.begin + a.chunk_tokens - 1) / a.chunk_tokens);
   return s;
+}
+
+// Places of a selection up to its last block at or before `last`.
+__device__ inline int32_t listed_of(const int32_t *sel, int32_t budget, int32_t last) {
+  constexpr int kAtOnce = 4;  // loads in flight
+  const int lane = threadIdx.x & 63;
+  for (int32_t top = budget; top > 0; top -= kAtOnce * kLanes) {
+    uint32_t e[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int32_t at = top - 1 - i * kLanes - lane;
+      e[i] = at < 0 ? ~0u : (uint32_t)sel[at];
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const uint64_t there = __ballot(e[i] <= (uint32_t)last);
+      if (there) return top - i * kLanes - __builtin_ctzll(there);
+    }
+  }
+  return 0;
 }
 
 // Largest value over the lanes that hold the same column of a 16-column

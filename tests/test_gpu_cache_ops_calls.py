@@ -191,3 +191,17 @@ def test_a_batch_s_calls_of_two_shapes():
     for _ in range(2):
         st.check(st.attend(), MANY)
         st.check(st.attend(selected=sel), FEW, selected=sel)
+
+
+# ------------------------------------------------- selections in any order
+
+@pytest.mark.parametrize("lead", [1, 2, 40, 300])
+@pytest.mark.parametrize("page", [16, 5])
+def test_blocks_that_follow_entries_that_are_none(lead, page):
+    # more skipped entries before the blocks than the sequence has blocks
+    st = Step([20, 70, 3, 150], [1, 2, 1, 3], 2, 3, 64, page=page)
+    blocks = st.choose(4)
+    none = torch.tensor([-1, 1 << 30, -7, 5000], dtype=torch.int32, device="cuda")
+    sel = none.repeat(lead)[:lead].expand(st.n_rows, st.H, lead)
+    sel = torch.cat([sel, blocks.flip(-1)], -1).contiguous()
+    st.check(st.attend(selected=sel), FEW, selected=sel)
