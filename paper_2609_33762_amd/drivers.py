@@ -272,16 +272,35 @@ class ServedTurns:
         return n, events
 
     def _store(self, keys, pages):
-        """The blocks that the tier does not hold yet; how many went."""
-        for tier, cache in self.pairs:
-            _, slots = tier.alloc(keys)
-            new = slots >= 0
-            if new.any():
-                try:
-                    tier.store(cache, pages[new], slots[new])
-                finally:
-                    tier.unpin(slots[new])
-        return int(new.sum())
+        """The blocks that the tiers do not hold yet; how many went.  A block
+        and its scales are one: where a tier still holds its half of a block
+        that another has lost, that half is written again, since codes made
+        along another path may need other scales."""
+        got, again = [], []  # each tier's slots (-1: none), and those that were resident
+        try:
+            for tier, _ in self.pairs:
+                got.append(tier.alloc(keys)[1])
+                again.append(np.zeros(len(keys), bool))
+            new = np.stack(got) >= 0
+            for i in np.flatnonzero(new.any(0) & ~new.all(0)):
+                for (tier, _), slots, old in zip(self.pairs, got, again):
+                    if slots[i] < 0:
+                        hit, slot = tier.lookup(keys[i:i + 1])
+                        if hit:
+                            slots[i], old[i] = slot[0], True
+            whole = (np.stack(got) >= 0).all(0)
+            # halves written again go first: their others, not stored yet, keep
+            # the block from being found should a store be refused
+            for resident in (True, False):
+                for (tier, cache), slots, old in zip(self.pairs, got, again):
+                    now = whole & (old == resident)
+                    if now.any():
+                        tier.store(cache, pages[now], slots[now])
+        finally:
+            for (tier, _), slots in zip(self.pairs, got):
+                if (slots >= 0).any():
+                    tier.unpin(slots[slots >= 0])
+        return int(whole.sum())
 
     def turn(self, prompt, n_new, pages):
         """prompt: int32 tokens; pages: pages for the prompt and n_new tokens,
