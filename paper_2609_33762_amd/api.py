@@ -299,7 +299,9 @@ class Batch:
     [n_seqs, pages], `kv_len` int32 [n_seqs] (tokens with the step's own),
     `row_start` int32 [n_seqs + 1] or None (one row each).  max_kv and
     max_rows bound what the device values hold.  Keeps the scratch of the
-    calls made with it, one buffer for each stream."""
+    calls made with it, one buffer for each stream, and every buffer that a
+    larger one replaced: a graph that captured a call uses its scratch as long
+    as the batch lives."""
 
     def __init__(self, page_table, kv_len, max_kv, row_start=None, n_rows=None, max_rows=None):
         if not page_table.is_cuda or str(page_table.dtype) != "torch.int32" or \
@@ -325,7 +327,7 @@ class Batch:
                                 page_table.stride(0) if n > 1 else self.pages, n, n_rows,
                                 max_rows, max_kv)
         self.ref, self.device = C.byref(self.desc), kv_len.device
-        self._need, self._scratch = {}, {}
+        self._need, self._scratch, self._replaced = {}, {}, []
 
     def need(self, shape, query, cache, args):
         """Workspace bytes of a call of this shape."""
@@ -348,6 +350,8 @@ class Batch:
             # taken on the calls' own stream: the allocator orders reuse by it
             with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
                 t = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+            if (call, stream) in self._scratch:
+                self._replaced.append(self._scratch[call, stream])
             self._scratch[call, stream] = t
         return t.data_ptr()
 

@@ -205,3 +205,39 @@ def test_blocks_that_follow_entries_that_are_none(lead, page):
     sel = none.repeat(lead)[:lead].expand(st.n_rows, st.H, lead)
     sel = torch.cat([sel, blocks.flip(-1)], -1).contiguous()
     st.check(st.attend(selected=sel), FEW, selected=sel)
+
+
+# ------------------------------------------------- captured calls
+
+def test_a_captured_call_keeps_its_scratch_when_a_larger_one_comes():
+    st = Step([9000], [100], 1, 8, 128)
+    sel = st.choose(64)
+    side = torch.cuda.Stream()
+    out, lse = torch.empty_like(st.q), torch.empty((100, 8), device="cuda")
+
+    def selected():
+        st.cache.attend(0, st.batch, st.q, out, selected=sel, lse=lse)
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        selected()
+    side.synchronize()
+    (small,) = (t.numel() for t in st.batch._scratch.values())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        selected()
+    with torch.cuda.stream(side):
+        st.check(st.attend(), MANY)  # needs more
+        assert max(t.numel() for t in st.batch._scratch.values()) > small
+        # what the allocator has of the first buffer's size
+        others = [torch.zeros(small, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    for _ in range(3):
+        out.fill_(math.nan)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        st.check((out, lse), FEW, selected=sel)
+        with torch.cuda.stream(side):
+            st.check(st.attend(), MANY)
+        torch.cuda.synchronize()
+        assert not any(bool(t.any()) for t in others)
