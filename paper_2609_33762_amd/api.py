@@ -229,9 +229,10 @@ class Cache:
         ref, s = C.byref(a), self._stream(stream)
         need = batch.need(("attend", self._shape, heads, window, budget),
                           self._lib.ea_attend_workspace, self._h, ref)
+        ws = batch.workspace("attend", need, s)
         N.check("ea_attend", self._lib.ea_attend(
-            self._h, self._planes_ref, layer, batch.ref, ref, batch.workspace("attend", need, s),
-            need, s))
+            self._h, self._planes_ref, layer, batch.ref, ref,
+            None if ws is None else ws.data_ptr(), need, s))
 
     def _selection(self, t, n_rows):
         _device_ints(t, "selected", self._device)
@@ -251,9 +252,10 @@ class Cache:
         ref, s = C.byref(a), self._stream(stream)
         need = batch.need(("select", self._shape, heads, budget, first, last),
                           self._lib.ea_select_workspace, self._h, ref)
+        ws = batch.workspace("select", need, s)
         N.check("ea_select_blocks", self._lib.ea_select_blocks(
-            self._h, self._planes_ref, layer, batch.ref, ref, batch.workspace("select", need, s),
-            need, s))
+            self._h, self._planes_ref, layer, batch.ref, ref,
+            None if ws is None else ws.data_ptr(), need, s))
 
 
 _ACT, _F32 = {}, []  # torch's dtypes, once a call has needed them
@@ -300,8 +302,10 @@ class Batch:
     `row_start` int32 [n_seqs + 1] or None (one row each).  max_kv and
     max_rows bound what the device values hold.  Keeps the scratch of the
     calls made with it, one buffer for each stream, and every buffer that a
-    larger one replaced: a graph that captured a call uses its scratch as long
-    as the batch lives."""
+    larger one replaced: a graph that captured a call uses its scratch, so the
+    batch has to outlive it.  A call captured on a stream that has no scratch
+    large enough takes the graph's own memory and clears its counters in every
+    replay; the same call made once before, on that stream, spares that."""
 
     def __init__(self, page_table, kv_len, max_kv, row_start=None, n_rows=None, max_rows=None):
         if not page_table.is_cuda or str(page_table.dtype) != "torch.int32" or \
@@ -340,8 +344,8 @@ class Batch:
         return n
 
     def workspace(self, call, nbytes, stream):
-        """Device scratch of at least nbytes for this call on this stream,
-        zero when it is new."""
+        """Device scratch of at least nbytes for this call on this stream (to
+        be held until it is launched), its counters zero when it is new."""
         if nbytes == 0:
             return None
         t = self._scratch.get((call, stream))
@@ -349,11 +353,20 @@ class Batch:
             import torch
             # taken on the calls' own stream: the allocator orders reuse by it
             with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
+                if torch.cuda.is_current_stream_capturing():
+                    # the graph's memory, zeroed in every replay and not
+                    # before the first: nothing for a call outside it
+                    t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+                    t[:_COUNTERS].zero_()
+                    return t
                 t = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
             if (call, stream) in self._scratch:
                 self._replaced.append(self._scratch[call, stream])
             self._scratch[call, stream] = t
-        return t.data_ptr()
+        return t
+
+
+_COUNTERS = 32 << 10  # bytes at an attention workspace's start, zero for a call
 
 
 def make_policy(kappa, block_tokens, beta_rank, theta_ppm=950000, activity_window=64,

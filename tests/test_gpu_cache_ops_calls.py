@@ -241,3 +241,45 @@ def test_a_captured_call_keeps_its_scratch_when_a_larger_one_comes():
             st.check(st.attend(), MANY)
         torch.cuda.synchronize()
         assert not any(bool(t.any()) for t in others)
+
+
+def test_scratch_of_a_call_that_was_captured_first():
+    # the clearing of a buffer that a capture made is recorded, not done
+    st = Step([9000, 300], [1, 1], 2, 4, 128)
+    out, lse = torch.empty_like(st.q), torch.empty((2, 8), device="cuda")
+    sel, ids = st.choose(100), torch.empty((2, 2, 7), dtype=torch.int32, device="cuda")
+    bounds = torch.randint(-9, 10, (1, 96, 2, 2, 128), dtype=torch.int8, device="cuda")
+    cache = api.Cache(st.kv, 96, 1, 16, 2, 128, 2, bounds=bounds.sort(2).values.contiguous(),
+                      bound_scales=torch.ones((1, 96, 2), device="cuda"))
+
+    def step():
+        cache.select_blocks(0, st.batch, st.q, ids)
+        cache.attend(0, st.batch, st.q, out, selected=sel, lse=lse)
+        cache.attend(0, st.batch, st.q, out, lse=lse)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step()
+    for t in st.batch._scratch.values():  # what fresh memory may hold
+        t.fill_(0x55)
+    torch.cuda.synchronize()
+    out.fill_(math.nan)
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    st.check((out, lse), FEW)
+    want = ids.clone()
+    for _ in range(3):
+        out.fill_(math.nan)
+        ids.fill_(9)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        st.check((out, lse), FEW)
+        assert torch.equal(ids, want)
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.synchronize()
+        st.check((out, lse), FEW)
