@@ -591,7 +591,7 @@ typedef struct {
   const int32_t *row_start;  /* int32[n_seqs+1] non-decreasing, or NULL       */
   int64_t table_stride;      /* * page_tokens >= max_kv                       */
   int32_t n_seqs;
-  int32_t n_rows;            /* rows of all sequences                         */
+  int32_t n_rows;            /* most rows of all sequences                    */
   int32_t max_rows;          /* most rows of one sequence                     */
   int32_t max_kv;            /* most kv_len; at most 2^30                     */
 } ea_batch;

@@ -181,7 +181,8 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_attention *a) {
   else if (a->window > 0)
     span = std::min<int64_t>(span, (int64_t)a->window + b->max_rows + ea::kChunkTokens);
   p.chunk = !a->selected && b->max_rows * G > cap;
-  // rows of a chunk that all sequences share leave nothing to the split kernel
+  // where all sequences may have the chunk's rows the split kernel is not
+  // launched, and the chunk kernel takes sequences of fewer rows too
   p.split = !p.chunk || (int64_t)b->n_seqs * b->max_rows != b->n_rows;
   p.splits = 1;
   p.chunk_tokens = (int32_t)up(std::max<int64_t>(span, 1) + ea::kChunkTokens, ea::kChunkTokens);
@@ -387,7 +388,7 @@ int ea_attend(ea_cache *c, const ea_cache_planes *planes, int32_t layer, const e
   k.window = a->window;
   k.group = a->q_heads / d.num_kv_heads;
   k.scale_log2 = a->scale * 1.4426950408889634f;
-  k.split_rows_most = ea::split_rows_cap(d.head_dim);
+  k.split_rows_most = p.split ? ea::split_rows_cap(d.head_dim) : 0;
   k.split_wgs = p.split_wgs;
   k.least_steps = p.least_steps;
   k.split_grid = p.split_grid;

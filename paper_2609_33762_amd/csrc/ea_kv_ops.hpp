@@ -62,7 +62,7 @@ struct AttendArgs {
   int32_t group;            // query heads per KV head
   float scale_log2;         // softmax scale times log2(e)
   // Sequences with at most this many rows times heads of a group go to the
-  // split kernel, others to the chunk kernel.
+  // split kernel (0: it is not launched), others to the chunk kernel.
   int32_t split_rows_most;
   // Split kernel: a workgroup takes heads_wg (1 or 2) neighbouring KV heads.
   // A unit (a sequence and as many heads) is split so that the parts of all

@@ -283,3 +283,17 @@ def test_scratch_of_a_call_that_was_captured_first():
             step()
         torch.cuda.synchronize()
         st.check((out, lse), FEW)
+
+
+# ------------------------------------------------- rows that only the device knows
+
+@pytest.mark.parametrize("rows,most", [([5], 128), ([0], 128), ([1], 300), ([3, 0, 100], 100),
+                                       ([2, 150, 60], 150)])
+def test_fewer_rows_than_the_host_was_told(rows, most):
+    # a step padded to its largest form: n_rows and max_rows are bounds
+    lens = [900 + 70 * i for i in range(len(rows))]
+    st = Step(lens, rows, 1, 8, 64, n_rows=most * len(rows), max_rows=most)
+    there = slice(0, sum(rows))
+    got = st.attend()
+    st.check(got, MANY, rows=there)
+    assert torch.isnan(got[0][sum(rows):]).all()  # rows of nobody are left as they are
