@@ -11,9 +11,10 @@
 //
 // fp8 keys and values become 16-bit values, exactly, on their way into LDS.
 // A key's scale multiplies its scores.  A value's scale, relative to the
-// largest one so far, multiplies its weight: both stay 32 bits until the
-// weight is rounded to f16, whose range the relative scale and the running
-// maximum hold.
+// largest one among the blocks that the row has seen so far, multiplies its
+// weight: both stay 32 bits until the weight is rounded to f16, whose range the
+// relative scale and the running maximum hold: down to 2^-29 of both a weight
+// keeps 11 bits, below 2^-40 it is gone.
 //
 // Measured: 2,048 rows of 4 KV heads of 8 over 26,624 16-bit tokens, 0.86
 // TFLOP, in 0.93 ms (0.93 PFLOP/s; a large library product reaches 1.3), ragged
@@ -111,9 +112,10 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
     }
   }
 
-  // O is held in units of v_scale / owed: a wave that skips a tile owes O the
-  // change of the unit
-  float m = kNegInf, l = 0.f, v_scale = 0.f, owed = 1.f;
+  // fp8: O is held in units of v_scale / owed, the change of the unit that O is
+  // still to be multiplied by.  A row's own: a unit shared with rows of other
+  // blocks would leave small scales beside a large one no bits.
+  float m = kNegInf, l = 0.f, v_scale = 0.f, v_inv = 0.f, owed = 1.f;
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -242,6 +244,14 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
     load(t0);
     if (TILES) look(t0 + kTok);
   }
+  // The rows' units grow to `top`, which is rare.
+  auto grow_units = [&](float top) {
+    if (!__any(top > v_scale)) return;
+    top = fmaxf(top, v_scale);
+    owed *= top > 0.f ? v_scale / top : 1.f;
+    v_scale = top;
+    v_inv = top >= 0x1p-126f ? 1.f / top : 0.f;
+  };
   // A weight of zero does not keep out what is not finite: in tiles of which
   // some row does not see all, such values count as zero and are left for the
   // end.
@@ -251,7 +261,9 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   for (int base = t0; base < t1; base += kTok) {
     const bool cut = gone || base < wg_all_low || base + kTok > wg_all_lim;
     __syncthreads();  // the last tile has been read
-    float ks[TP], vs[TP];  // TILES: of 16 tokens each; else in LDS
+    // TILES: of 16 tokens each; else in LDS, those of values as they are, `most`
+    // the largest
+    float ks[TP], vs[TP], most = 0.f;
     if (FP8) {
       if (cut) {
 #pragma unroll
@@ -260,22 +272,30 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
           v_sc[t] = finite(v_sc[t]) ? v_sc[t] : 0.f;
         }
       }
-      float top = v_scale;
 #pragma unroll
-      for (int t = 0; t < (TILES ? TP : 1); ++t) top = fmaxf(top, fabsf(v_sc[t]));
-      if (!TILES)
-        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      if (top > v_scale) owed *= v_scale / top;
-      v_scale = top;
-      const float inv = top >= 0x1p-126f ? 1.f / top : 0.f;
-#pragma unroll
-      for (int t = 0; t < TP; ++t) {
-        ks[t] = k_sc[TILES ? t : 0] * a.scale_log2;
-        vs[t] = v_sc[TILES ? t : 0] * inv;
+      for (int t = 0; t < (TILES ? TP : 1); ++t) {
+        ks[t] = k_sc[t] * a.scale_log2;
+        vs[t] = v_sc[t];
       }
-      if (!TILES && wave == 0) {
-        ks_lds[lane] = ks[0];
-        vs_lds[lane] = vs[0];
+      if constexpr (TILES) {
+        if (cut) {  // of blocks that the row does not see a token of
+#pragma unroll
+          for (int t = 0; t < TP; ++t)
+            vs[t] = base + t * 16 < lim && base + t * 16 + 16 > low ? vs[t] : 0.f;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int t = 0; t < TP; ++t) top = fmaxf(top, fabsf(vs[t]));
+        grow_units(top);
+#pragma unroll
+        for (int t = 0; t < TP; ++t) vs[t] *= v_inv;
+      } else {
+        most = fabsf(vs[0]);
+        for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+        if (wave == 0) {
+          ks_lds[lane] = ks[0];
+          vs_lds[lane] = vs[0];
+        }
       }
     }
 #pragma unroll
@@ -359,6 +379,22 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
           for (int i = 0; i < 4; ++i) x[t][q * 4 + i] *= f[i];
         }
     }
+    if constexpr (FP8 && !TILES) {
+      if (cut) {  // of the tokens that the row sees
+        most = 0.f;
+#pragma unroll 1  // the scales are read again below: no registers for them
+        for (int q = 0; q < 8; ++q) {
+          const f32x4 f = *reinterpret_cast<const f32x4 *>(vs_lds + q * 8 + gg * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = base + q * 8 + gg * 4 + i;
+            most = fmaxf(most, at >= low && at < lim ? fabsf(f[i]) : 0.f);
+          }
+        }
+        most = max_rows32(most);
+      }
+      grow_units(most);
+    }
     const float unit = FP8 ? 1.f : a.scale_log2;  // of a score, in powers of two
     if (gone_here || base < all_low || base + kTok > all_lim) {
 #pragma unroll
@@ -377,10 +413,10 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
       for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
     top = max_rows32(top);
     const float ref = top == kNegInf ? 0.f : top * unit - kShift;
-    if (__any(top != m) || owed != 1.f) {
+    if (__any(FP8 ? top != m || owed != 1.f : top != m)) {
       const float f = m == kNegInf ? 0.f : exp2_fast(m * unit - kShift - ref);
       l *= f;
-      const float fo = f * owed;
+      const float fo = FP8 ? f * owed : f;
       owed = 1.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -406,7 +442,14 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
           l += p[i];
         }
         if (FP8) {
-          const f32x4 f = scale_of(vs_lds, vs, t, q);
+          f32x4 f = scale_of(vs_lds, vs, t, q);
+          if constexpr (!TILES) {
+            f *= v_inv;
+            // tokens that the row does not see may have any (finite) scale
+            if (cut)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_fmed3f(f[i], -1.f, 1.f);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] *= f[i];
         }
@@ -459,7 +502,8 @@ __global__ __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) void attend_chunk(Attend
   const float unit = FP8 ? 1.f : a.scale_log2;
   const float ref = m == kNegInf ? kNegInf : m * unit - kShift;
   const int64_t row = sq.row0 + qi, head = h * G + r % G;
-  const float out_scale = FP8 ? v_scale * owed : 1.f;
+  // (v_scale 0: only what is not finite has been added)
+  const float out_scale = FP8 && v_scale > 0.f ? v_scale * owed : 1.f;
   if (span.parts == 1) {
     const float f = total == 0.f ? 0.f : out_scale / total;
     uint16_t *op = a.out.data + row * a.out.row_stride + head * a.out.head_stride;

@@ -297,3 +297,25 @@ def test_fewer_rows_than_the_host_was_told(rows, most):
     got = st.attend()
     st.check(got, MANY, rows=there)
     assert torch.isnan(got[0][sum(rows):]).all()  # rows of nobody are left as they are
+
+
+# ------------------------------------------------- scales of blocks that some rows see
+
+@pytest.mark.parametrize("rows,group,dim", [(70, 4, 64), (100, 2, 128), (140, 1, 80), (40, 2, 256)])
+@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("far", [2.0 ** 12, 2.0 ** 60])
+def test_a_large_scale_that_other_rows_of_a_chunk_see(rows, group, dim, page, window, far):
+    # values of the last block, and of one in the middle, are far larger than
+    # the others: rows that attend to neither lose nothing
+    n = rows + 30
+    st = base.Setup(kv_lens=[n, 90], rows=[rows, 3], heads=2, group=group, dim=dim, page=page,
+                    fp8=True)
+    for token in (n - 1, n - rows // 2):
+        st.scales[st.layer, int(st.table[0, token // page]), 1] *= far
+    st.d_scales.copy_(st.scales.cuda())
+    q = st.rand(2 * group)
+    out = torch.full_like(q, math.nan, device="cuda")
+    lse = torch.empty((st.n_rows, 2 * group), device="cuda")
+    st.handle.attend(st.layer, st.batch, q.cuda(), out, window=window, lse=lse)
+    base.check_attention(st, q, out, lse, st.D ** -0.5, 2.0 ** -11, window=window)
