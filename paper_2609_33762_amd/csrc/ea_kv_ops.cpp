@@ -329,8 +329,9 @@ int ea_append_kv(ea_cache *c, const ea_cache_planes *planes, int32_t layer, cons
   k.fp8 = d.elem_bytes == 1;
   k.pages_most = (int32_t)((b->max_rows + (int64_t)d.page_tokens - 2) / d.page_tokens + 1);
   const int64_t units = (int64_t)b->n_seqs * k.pages_most;
+  const int64_t queries = a->q.data ? (int64_t)b->n_rows * (a->q_heads / 16 + 1) : 0;
   if (units > INT32_MAX / (2LL * d.num_kv_heads) ||
-      units * 2 * d.num_kv_heads + (int64_t)b->n_rows * (a->q_heads / 16 + 1) > INT32_MAX)
+      units * 2 * d.num_kv_heads + queries > INT32_MAX)
     return EA_ENOTSUP;
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());

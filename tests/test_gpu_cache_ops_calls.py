@@ -319,3 +319,20 @@ def test_a_large_scale_that_other_rows_of_a_chunk_see(rows, group, dim, page, wi
     lse = torch.empty((st.n_rows, 2 * group), device="cuda")
     st.handle.attend(st.layer, st.batch, q.cuda(), out, window=window, lse=lse)
     base.check_attention(st, q, out, lse, st.D ** -0.5, 2.0 ** -11, window=window)
+
+
+# ------------------------------------------------- appends without queries
+
+def test_an_append_without_queries_asks_nothing_of_their_number():
+    lib, ref = N.load(), C.byref
+    st = Step([40], [20], 2, 2, 64)
+    k, v = (torch.randn((20, 2, 64), generator=st.g).to(BF16).cuda() for _ in range(2))
+    rows = [N.Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (k, v)]
+    a = N.Append(*rows)
+    a.q_heads, a.dtype = 0x7FFFFFFF, N.EA_BF16  # q.data is NULL
+    st.table[0] = torch.arange(3, dtype=torch.int32)
+    N.check("ea_append_kv", lib.ea_append_kv(st.cache.handle, ref(N.CachePlanes(None, None, None)), 0,
+                                             st.batch.ref, ref(a), api.current_stream()))
+    torch.cuda.synchronize()
+    got = st.kv[0, :3].transpose(0, 1).reshape(2, 48, 2, 64)[:, 20:40]
+    assert torch.equal(got[0], k) and torch.equal(got[1], v)
