@@ -324,9 +324,7 @@ class ServedTurns:
         for layer in range(cache.num_layers):
             if held:
                 torch.cuda.current_stream(self.device).wait_event(events[layer])
-                if cache.bounds is not None:
-                    cache.bound_blocks(restored, layer, 1, dtype=x.dtype)
-            x = self._layer(layer, batch, x)
+            x = self._layer(layer, batch, x, restored=restored if held else None)
 
         # new tokens, one by one; the last one made is not in the cache
         length, made = self._ints([n]), []
@@ -347,9 +345,12 @@ class ServedTurns:
         stored = self._store(keys[held:], pages[held:len(keys)]) if len(keys) > held else 0
         return made, held, stored
 
-    def _layer(self, layer, batch, x, chosen=None):
+    def _layer(self, layer, batch, x, chosen=None, restored=None):
         cache = self.cache
         q, k, v = self.model.project(layer, x)
+        if restored is not None and cache.bounds is not None:
+            # k has the type of a 16-bit cache's blocks; x may have any
+            cache.bound_blocks(restored, layer, 1, dtype=k.dtype)
         turned = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
         cache.append_kv(layer, batch, k, v, rope=self.rope, q=q, q_out=turned)
         if chosen is not None:

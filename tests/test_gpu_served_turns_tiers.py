@@ -49,3 +49,36 @@ def test_a_block_comes_back_with_the_scales_it_was_made_with(block_slots, scale_
     assert (scales[:, made] > 0).all()
     assert torch.equal(kv[:, made].view(torch.uint8), kv[:, back].view(torch.uint8))
     assert torch.equal(scales[:, made], scales[:, back])
+
+
+@pytest.mark.parametrize("act,x_dtype", [(base.BF16, torch.float32), (base.F16, torch.bfloat16)])
+def test_bounds_of_restored_blocks_go_by_the_cache_s_type(act, x_dtype):
+    # x may have any type: the bounds are of what the blocks hold
+    need_gpu()
+
+    class Mixed(served.Model):
+        def embed(self, tokens):
+            return super().embed(tokens).to(x_dtype)
+
+        def project(self, layer, x):
+            return tuple(t.to(act) for t in super().project(layer, x.to(base.BF16)))
+
+        def mix(self, layer, x, attention):
+            return super().mix(layer, x.to(base.BF16), attention.to(base.BF16)).to(x_dtype)
+
+    kv = torch.zeros((L, P, 2, T, H, D), dtype=act, device="cuda")
+    bounds = torch.zeros((L, P, 2, H, D), dtype=torch.int8, device="cuda")
+    units = torch.zeros((L, P, H), device="cuda")
+    cache = api.Cache(kv, P, L, T, H, D, 2, bounds=bounds, bound_scales=units)
+    serve = ServedTurns(torch, cache, api.Tier(cache, 32 * cache.slot_bytes), Mixed(), 4,
+                        rope=base.rope_table(400, D).cuda())
+    r = np.random.default_rng(7)
+    prompt = r.integers(0, VOCAB, 90).astype(np.int32)
+    pages = r.permutation(P).astype(np.int32)
+    assert serve.turn(prompt, 3, pages[:6])[1] == 0
+    assert serve.turn(prompt, 3, pages[6:12])[1] == 5
+    torch.cuda.synchronize()
+    made, back = (torch.as_tensor(pages[a:a + 5], device="cuda").long() for a in (0, 6))
+    assert torch.equal(kv[:, made], kv[:, back]) and bool((units[:, made] > 0).all())
+    assert torch.equal(bounds[:, made], bounds[:, back])
+    assert torch.equal(units[:, made], units[:, back])
