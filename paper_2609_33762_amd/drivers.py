@@ -306,6 +306,15 @@ class ServedTurns:
         """prompt: int32 tokens; pages: pages for the prompt and n_new tokens,
         the caller's, free of any transfer.  Returns the tokens made, the
         blocks restored and the blocks stored."""
+        try:
+            return self._turn(prompt, n_new, pages)
+        except BaseException:
+            # blocks on their way still go to these pages: what follows on this
+            # stream waits for them
+            self.torch.cuda.current_stream(self.device).wait_stream(self.copy_stream)
+            raise
+
+    def _turn(self, prompt, n_new, pages):
         torch, cache, model, T = self.torch, self.cache, self.model, self.T
         prompt, pages = np.asarray(prompt, np.int32), np.asarray(pages, np.int32)
         n = len(prompt)

@@ -82,3 +82,28 @@ def test_bounds_of_restored_blocks_go_by_the_cache_s_type(act, x_dtype):
     assert torch.equal(kv[:, made], kv[:, back]) and bool((units[:, made] > 0).all())
     assert torch.equal(bounds[:, made], bounds[:, back])
     assert torch.equal(units[:, made], units[:, back])
+
+
+def test_pages_of_a_turn_that_failed_are_free_of_transfers():
+    cache, model, serve = served.setting(False, 4)
+    r = np.random.default_rng(8)
+    prompt = r.integers(0, VOCAB, 90).astype(np.int32)
+    pages = r.permutation(P).astype(np.int32)
+    assert serve.turn(prompt, 1, pages[:6])[1:] == (0, 5)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(serve.copy_stream):
+        torch.cuda._sleep(100_000_000)  # the blocks come late
+    embed = model.embed
+
+    def fails(tokens):
+        raise RuntimeError("of the model")
+
+    model.embed = fails
+    with pytest.raises(RuntimeError, match="of the model"):
+        serve.turn(prompt, 1, pages[6:12])
+    again = torch.as_tensor(pages[6:12], device="cuda").long()
+    cache.kv[:, again] = 7.0
+    torch.cuda.synchronize()
+    assert bool((cache.kv[:, again] == 7.0).all())
+    model.embed = embed
+    assert serve.turn(prompt, 1, pages[6:12])[1:] == (5, 0)
