@@ -336,3 +336,50 @@ def test_an_append_without_queries_asks_nothing_of_their_number():
     torch.cuda.synchronize()
     got = st.kv[0, :3].transpose(0, 1).reshape(2, 48, 2, 64)[:, 20:40]
     assert torch.equal(got[0], k) and torch.equal(got[1], v)
+
+
+# ------------------------------------------------- selections of many blocks
+
+@pytest.mark.parametrize("blocks,budget,first,last", [
+    (1024, 100, 1, 1), (1025, 1000, 1, 2), (4096, 64, 0, 0), (4097, 300, 2, 1), (16384, 77, 1, 1),
+    (16385, 5000, 1, 1), (65536, 128, 1, 1)])
+@pytest.mark.parametrize("spread", [100, 2])  # few values: many ties
+def test_selections_of_many_blocks(blocks, budget, first, last, spread):
+    need_gpu()
+    g = torch.Generator().manual_seed(blocks + spread)
+    H, G, D = 2, 3, 24
+    lens = [blocks, blocks - 3, min(blocks, budget + 1), max(1, budget // 2)]
+    P = 500
+    kv = torch.zeros((1, P, 2, 1, H, D), dtype=BF16, device="cuda")
+    lo, hi = (torch.randint(0, spread + 1, (1, P, H, D), generator=g) * (1 if spread > 2 else 40)
+              for _ in range(2))
+    bounds = torch.stack([-lo, hi], 2).to(torch.int8).cuda()
+    units = torch.exp2(torch.randint(-2, 3, (1, P, H), generator=g).float()).cuda()
+    table = torch.randint(-1, P + 1, (len(lens), blocks), generator=g, dtype=torch.int32)
+    cache = api.Cache(kv, P, 1, 1, H, D, 2, bounds=bounds, bound_scales=units)
+    batch = api.Batch(table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), blocks)
+    q = torch.randn((len(lens), H * G, D), generator=g).to(BF16)
+    got = torch.full((len(lens), H, budget), 9, dtype=torch.int32, device="cuda")
+    cache.select_blocks(0, batch, q.cuda(), got, first=first, last=last)
+
+    b, u = bounds[0].cpu().double(), units[0].cpu().double()
+    for s, held in enumerate(lens):
+        ids = table[s, :held].long()
+        there = (ids >= 0) & (ids < P)
+        pages = torch.where(there, ids, 0)
+        for h in range(H):
+            best = torch.full((held,), -math.inf, dtype=torch.float64)
+            for j in range(G):
+                x = q[s, h * G + j].double()
+                unit = base.power(float(x.abs().max()), 127.0)
+                c = (x / unit).round()
+                score = torch.maximum(c * b[pages, 0, h], c * b[pages, 1, h]).sum(-1)
+                best = torch.maximum(best, score * unit * u[pages, h])
+            # pages that are not there come last, forced blocks first
+            best = torch.where(there, best, -math.inf)
+            at = torch.arange(held)
+            best = torch.where((at < first) | (at >= held - last), math.inf, best)
+            order = torch.sort(best, descending=True, stable=True).indices[:budget]
+            want = torch.full((budget,), -1, dtype=torch.int32)
+            want[:len(order)] = order.sort().values.int()
+            assert torch.equal(got[s, h].cpu(), want), (s, h)
