@@ -661,8 +661,12 @@ typedef struct {
 /* Attention of a step's queries over layer `layer`: row r of sequence s, at
  * position p = kv_len[s] - rows + r, attends to the tokens j <= p of its
  * sequence (j > p - window; in its selected blocks), query head i to KV head
- * i / (q_heads / H).  Sums and softmax statistics are 32 bits.  A row that
- * attends to nothing gets zeros.  What lies in tokens that a row does not
+ * i / (q_heads / H).  Sums and softmax statistics are 32 bits; the weights that
+ * multiply the values are rounded, by the kernel that takes the sequence.  Up to
+ * 64 rows times heads of a group (16 where head_dim > 128): to 16 bits, beside
+ * f16 values to 11.  More, and all sequences of a call where n_seqs * max_rows is
+ * n_rows and max_rows has more: to 8 bits beside bf16 values, to 11 beside f16 and
+ * fp8 ones.  A row that attends to nothing gets zeros.  What lies in tokens that a row does not
  * attend to never reaches it, be it infinite or NaN, and neither do scales of
  * blocks that it has no token of.  workspace (16-byte aligned device
  * memory, ea_attend_workspace bytes; NULL when that is 0) is scratch of this

@@ -9,6 +9,13 @@
 // exchange with the lane 32 away, and P goes from the scores' registers into
 // the second product as it is.  V^T comes from LDS through transposing reads.
 //
+// P goes into the second product as one 16-bit value of the type beside it: 8
+// bits for bf16 values (the split kernel, whose matrix units idle, takes two),
+// 11 for f16 and fp8 ones.  A second product for the rest of P would be half as
+// many matrix instructions again in a kernel that they bound.  Against 64 bits
+// the chunk below is 0.0023 off (2-norm) where rounding the result alone gives
+// 0.0017.  The sums of weights are of the unrounded ones, in 32 bits.
+//
 // fp8 keys and values become 16-bit values, exactly, on their way into LDS.
 // A key's scale multiplies its scores.  A value's scale, relative to the
 // largest one among the blocks that the row has seen so far, multiplies its
@@ -17,9 +24,11 @@
 // keeps 11 bits, below 2^-40 it is gone.
 //
 // Measured: 2,048 rows of 4 KV heads of 8 over 26,624 16-bit tokens, 0.86
-// TFLOP, in 0.93 ms (0.93 PFLOP/s; a large library product reaches 1.3), ragged
-// fp8 chunks of 0.22 TFLOP in 0.42 ms.  Per tile the softmax takes about as
-// many cycles of a SIMD as the products, and two waves a SIMD hide it in part.
+// TFLOP, in 0.92 to 0.95 ms (0.93 PFLOP/s; a large library product reaches
+// 1.3), ragged fp8 chunks of 0.22 TFLOP in 0.41 ms.  By counters a SIMD's matrix
+// unit is busy for 39% of the former's time and its vector unit for 37%: the
+// softmax between the products costs what they do, and two waves a SIMD hide it
+// in part.  The ragged chunks' compute units have work for 75% of the time.
 #include <hip/hip_runtime.h>
 
 #include "ea_kv_device.hpp"

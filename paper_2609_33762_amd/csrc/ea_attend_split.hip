@@ -28,7 +28,7 @@
 // f16 (11 bits) held at up to 2^15, so that small weights keep their bits.
 //
 // Measured: 64 sequences of 8,192-65,536 fp8 tokens, one KV head of 8, 623 MB
-// in 113 us (5.5 TB/s; reading random pages alone reaches 6.0); one sequence
+// in 114 us (5.5 TB/s; reading random pages alone reaches 6.0); one sequence
 // of 4 KV heads and 65,536 16-bit tokens, 134 MB, in 33 us, of which some 10
 // are the launch, the first loads' latency and the join.
 #include <hip/hip_runtime.h>
@@ -723,7 +723,7 @@ constexpr int kJoinWaves = 4;
 
 // Join of the chunk kernel's parts: one wave a row and head, a lane four
 // elements.  It reads the parts once, a launch of its own after the products
-// (18 us of 417 for six ragged fp8 chunks).
+// (18 us of 407 for six ragged fp8 chunks).
 template <int ACT>
 __global__ __launch_bounds__(kJoinWaves *kLanes) void attend_join(AttendArgs a) {
   const int HQ = a.kv.heads * a.group, D = a.kv.head_dim;
