@@ -241,7 +241,7 @@ class ServedTurns:
                  scale_tier=None, max_tokens=65536):
         if tier.chunk_pages != 1 or (scale_tier is not None and scale_tier.chunk_pages != 1):
             raise ValueError("served turns keep one page in a slot")
-        if (cache.head_scales is None) != (scale_cache is None):
+        if not (cache.head_scales is None) == (scale_cache is None) == (scale_tier is None):
             raise ValueError("head_scales need a scale_cache and a scale_tier, and only they do")
         self.torch, self.cache, self.model = torch, cache, model
         self.budget, self.rope = budget, rope

@@ -3,6 +3,7 @@ two tiers, on tiers that stand for the library's (metadata alone, no GPU):
 whatever a tier evicts and whichever store is refused, a block that both tiers
 hold has both halves from the same turn."""
 import itertools
+import types
 
 import numpy as np
 import pytest
@@ -132,3 +133,13 @@ def test_a_refused_store_leaves_no_block_of_two_turns(which, nth):
     t.pairs[which][0].refuse = 0
     store(t, [1, 2, 7], 4)
     assert set(whole(t)) >= {1, 2, 7}
+
+
+@pytest.mark.parametrize("plane,cache,tier", [(1, 1, 0), (1, 0, 1), (1, 0, 0), (0, 1, 1), (0, 0, 1),
+                                              (0, 1, 0)])
+def test_scales_without_their_cache_or_tier_are_refused(plane, cache, tier):
+    one_page = types.SimpleNamespace(chunk_pages=1)
+    given = types.SimpleNamespace(head_scales=object() if plane else None)
+    with pytest.raises(ValueError):
+        ServedTurns(None, given, one_page, None, 4, scale_cache=object() if cache else None,
+                    scale_tier=one_page if tier else None)
