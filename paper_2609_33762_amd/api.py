@@ -303,7 +303,8 @@ class Batch:
     max_rows bound what the device values hold.  Keeps the scratch of the
     calls made with it, one buffer for each stream, and every buffer that a
     larger one replaced: a graph that captured a call uses its scratch, so the
-    batch has to outlive it.  A call captured on a stream that has no scratch
+    batch has to outlive it, and what shares a stream's buffer (its calls, the
+    graphs captured on it) must not run at the same time.  A call captured on a stream that has no scratch
     large enough takes the graph's own memory and clears its counters in every
     replay; the same call made once before, on that stream, spares that."""
 
