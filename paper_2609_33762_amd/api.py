@@ -304,9 +304,10 @@ class Batch:
     calls made with it, one buffer for each stream, and every buffer that a
     larger one replaced: a graph that captured a call uses its scratch, so the
     batch has to outlive it, and what shares a stream's buffer (its calls, the
-    graphs captured on it) must not run at the same time.  A call captured on a stream that has no scratch
-    large enough takes the graph's own memory and clears its counters in every
-    replay; the same call made once before, on that stream, spares that."""
+    graphs captured on it) must not run at the same time.  A call captured on
+    a stream that has no scratch large enough takes the graph's own memory and
+    clears its counters in every replay; the same call made once before, on
+    that stream, spares that."""
 
     def __init__(self, page_table, kv_len, max_kv, row_start=None, n_rows=None, max_rows=None):
         if not page_table.is_cuda or str(page_table.dtype) != "torch.int32" or \
