@@ -706,6 +706,52 @@ int ea_select_blocks(ea_cache *cache, const ea_cache_planes *planes, int32_t lay
                      const ea_batch *batch, const ea_selection *args, void *workspace,
                      int64_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------- latent caches
+ *
+ * A cache of latents (not in the paper) holds one row of latent_dim + rope_dim
+ * elements for each token in place of keys and values: a latent that all heads
+ * share, and a key part that turns with the position.  It is an ea_cache of
+ * num_kv_heads 1 and head_dim (latent_dim + rope_dim) / 2, whose pieces are
+ * read as [page_tokens][latent_dim + rope_dim], so it goes to a tier, and from
+ * page to page, as any other.  elem_bytes 2 holds the rows' type; elem_bytes 1
+ * fp8 e4m3 with the cache's scale plane [L][P][2], one scale for the latents of
+ * a block and one for its turned parts.  latent_dim and rope_dim must be
+ * multiples of 16, at most 512 and 64 (EA_ENOTSUP otherwise).
+ *
+ * The batch, and what holds for device values, are as for the other cache
+ * operators. */
+
+typedef struct {
+  ea_rows q;           /* [n_rows][q_heads][latent_dim + rope_dim]: a head's
+                          query against latents (its part before rotation times
+                          the head's key weights), then its rotated part      */
+  ea_rows out;         /* [n_rows][q_heads][latent_dim]: sums of latents, which
+                          the head's value weights turn into its output       */
+  float *lse;          /* float32 [n_rows][q_heads] or NULL: natural log of
+                          the sum of exponentials, -inf for an empty row      */
+  int32_t latent_dim, rope_dim;
+  int32_t q_heads;
+  int32_t dtype;       /* ea_dtype of q and out                               */
+  float scale;         /* softmax scale, > 0 and finite: that of a head before
+                          its weights went into the query                     */
+  int32_t _pad;
+} ea_latent_attention;
+
+/* Attention of a step's queries over latents of layer `layer`: row r of
+ * sequence s, at position p = kv_len[s] - rows + r, attends with every head to
+ * the tokens j <= p of its sequence; a token's key is its whole row, its value
+ * its latent.  Sums and softmax statistics are 32 bits; the weights that
+ * multiply the latents are rounded to 11 bits beside f16 and fp8 latents, and
+ * beside bf16 ones to 16 bits in calls of up to 64 rows times heads a sequence
+ * (max_rows * q_heads), to 8 in others.  A row that attends to nothing gets
+ * zeros.  What lies in tokens that a row does not attend to never reaches it.
+ * workspace: as for ea_attend, ea_attend_latent_workspace bytes. */
+int64_t ea_attend_latent_workspace(const ea_cache *cache, const ea_batch *batch,
+                                   const ea_latent_attention *args);
+int ea_attend_latent(ea_cache *cache, int32_t layer, const ea_batch *batch,
+                     const ea_latent_attention *args, void *workspace,
+                     int64_t workspace_bytes, hipStream_t stream);
+
 /* How stores and loads cross the host link:
  *  EA_PLAN_DIRECT: one kernel reads/writes the mapped pinned slots;
  *  EA_PLAN_STAGED: gather/scatter through an HBM staging buffer plus DMA

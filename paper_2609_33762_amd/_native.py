@@ -104,6 +104,12 @@ class Selection(C.Structure):
                 ("dtype", C.c_int32), ("_pad", C.c_int32)]
 
 
+class LatentAttention(C.Structure):
+    _fields_ = [("q", Rows), ("out", Rows), ("lse", C.c_void_p), ("latent_dim", C.c_int32),
+                ("rope_dim", C.c_int32), ("q_heads", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float), ("_pad", C.c_int32)]
+
+
 class ControllerStatus(C.Structure):
     _fields_ = [("now", C.c_int64), ("reports_published", C.c_int64),
                 ("published", TierReport), ("seen", TierReport),
@@ -153,6 +159,8 @@ SIGNATURES = {
     "ea_attend": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
     "ea_select_workspace": (_I64, [_P, _P, _P]),
     "ea_select_blocks": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
+    "ea_attend_latent_workspace": (_I64, [_P, _P, _P]),
+    "ea_attend_latent": (_INT, [_P, _I32, _P, _P, _P, _I64, _P]),
     "ea_tier_set_plan": (_INT, [_P, _INT, _INT]),
     "ea_tier_get_plan": (_INT, [_P, _INT, _P]),
     "ea_peak_probe": (_INT, [_P, _P, _I64, _INT, _INT, _P]),

@@ -157,12 +157,13 @@ class Cache:
         if batch.device != self._device:
             raise ValueError("the batch lies on another device than the cache")
 
-    def _rows(self, t, what, n_rows, heads, act):
+    def _rows(self, t, what, n_rows, heads, act, dim=None):
         """Address and strides of rows [n_rows, heads, D]."""
         shape, stride = t.shape, t.stride()
+        dim = self.head_dim if dim is None else dim
         if len(shape) != 3 or shape[0] < n_rows or shape[1] != heads or \
-                shape[2] != self.head_dim or stride[2] != 1 or t.device != self._device:
-            raise ValueError(f"{what} must be a tensor [{n_rows}, {heads}, {self.head_dim}] on the "
+                shape[2] != dim or stride[2] != 1 or t.device != self._device:
+            raise ValueError(f"{what} must be a tensor [{n_rows}, {heads}, {dim}] on the "
                              "cache's device whose last dimension is contiguous")
         if _dtype(t) != act:
             raise ValueError(f"{what} must have the dtype of the call's other rows")
@@ -219,11 +220,7 @@ class Cache:
             budget = self._selection(selected, n)
             a.selected, a.budget = selected.data_ptr(), budget
         if lse is not None:
-            if lse.device != self._device or lse.dtype not in _f32() or \
-                    not lse.is_contiguous() or tuple(lse.shape) != (n, heads):
-                raise ValueError("lse must be a contiguous float32 tensor [n_rows, q_heads] on "
-                                 "the cache's device")
-            a.lse = lse.data_ptr()
+            a.lse = self._lse(lse, n, heads)
         a.window, a.q_heads, a.dtype = window, heads, act
         a.scale = self.head_dim ** -0.5 if scale is None else scale
         ref, s = C.byref(a), self._stream(stream)
@@ -233,6 +230,13 @@ class Cache:
         N.check("ea_attend", self._lib.ea_attend(
             self._h, self._planes_ref, layer, batch.ref, ref,
             None if ws is None else ws.data_ptr(), need, s))
+
+    def _lse(self, lse, n, heads):
+        if lse.device != self._device or lse.dtype not in _f32() or \
+                not lse.is_contiguous() or tuple(lse.shape) != (n, heads):
+            raise ValueError("lse must be a contiguous float32 tensor [n_rows, q_heads] on "
+                             "the cache's device")
+        return lse.data_ptr()
 
     def _selection(self, t, n_rows):
         _device_ints(t, "selected", self._device)
@@ -256,6 +260,50 @@ class Cache:
         N.check("ea_select_blocks", self._lib.ea_select_blocks(
             self._h, self._planes_ref, layer, batch.ref, ref,
             None if ws is None else ws.data_ptr(), need, s))
+
+
+class LatentCache(Cache):
+    """A caller-owned paged cache of latents: `kv` is a CUDA tensor holding
+    [L][P][T][latent_dim + rope_dim] elements (any dtype, contiguous), fp8 with
+    `scales` [L][P][2], those of a block's latents and of its turned parts.
+    Stored, loaded and copied as any cache; append_latent and attend_latent
+    are its operators in place of those of keys and values."""
+
+    def __init__(self, kv, num_pages, num_layers, page_tokens, latent_dim, rope_dim, elem_bytes,
+                 scales=None):
+        if (latent_dim + rope_dim) % 2:
+            raise ValueError("latent_dim + rope_dim must be even")
+        super().__init__(kv, num_pages, num_layers, page_tokens, 1, (latent_dim + rope_dim) // 2,
+                         elem_bytes, scales=scales)
+        self.latent_dim, self.rope_dim = latent_dim, rope_dim
+        self._shape = ("latent", latent_dim, rope_dim, page_tokens, elem_bytes)
+
+    def _keys_and_values(self, *args, **kwargs):
+        raise TypeError("a cache of latents holds no keys and values: append_latent and "
+                        "attend_latent are its operators")
+
+    append_kv = attend = select_blocks = bound_blocks = _keys_and_values
+
+    def attend_latent(self, layer, batch, q, out, scale, lse=None, stream=None):
+        """Attention of absorbed queries q [n_rows, q_heads, latent_dim +
+        rope_dim] over the cached tokens up to each row's own, into out
+        [n_rows, q_heads, latent_dim]; scale: of a head before absorption; lse:
+        float32 [n_rows, q_heads] output."""
+        self._fits(batch)
+        act, n, heads = _dtype(q), batch.n_rows, q.shape[1]
+        a = N.LatentAttention(
+            self._rows(q, "q", n, heads, act, self.latent_dim + self.rope_dim),
+            self._rows(out, "out", n, heads, act, self.latent_dim))
+        if lse is not None:
+            a.lse = self._lse(lse, n, heads)
+        a.latent_dim, a.rope_dim, a.q_heads, a.dtype = self.latent_dim, self.rope_dim, heads, act
+        a.scale = scale
+        ref, s = C.byref(a), self._stream(stream)
+        need = batch.need(("latent", self._shape, heads), self._lib.ea_attend_latent_workspace,
+                          self._h, ref)
+        ws = batch.workspace("attend", need, s)
+        N.check("ea_attend_latent", self._lib.ea_attend_latent(
+            self._h, layer, batch.ref, ref, None if ws is None else ws.data_ptr(), need, s))
 
 
 _ACT, _F32 = {}, []  # torch's dtypes, once a call has needed them

@@ -1,0 +1,795 @@
+// Attention over a cache of latents: of absorbed queries, whose keys are a
+// token's whole row (latent and turned part) and whose values are its latent.
+//
+//   o = sum_j p_j c_j / sum_j p_j,  p_j = 2^(x_j - m),
+//   x_j = scale log2(e) (q_c . c_j + q_r . r_j),  m a reference near the maximum
+//
+// All query heads share a token's row, so the rows of a matrix product are
+// query rows times heads, and a cached byte feeds both products.
+#include <hip/hip_runtime.h>
+
+#include "ea_kv_device.hpp"
+#include "ea_kv_parts.hpp"
+
+namespace ea {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kLanes;
+constexpr int kTurn = 64;      // elements of a row's turned part that the registers hold
+constexpr int kRing = 147456;  // most bytes of tokens in LDS
+
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// 16 bytes a lane from base + off (from p) to LDS, lane by lane from `at` on.
+// The load writes no register, and the compiler does not know of it: whoever
+// reads the bytes waits for it (vmcnt).
+__device__ inline void to_lds(uint32_t at, const uint8_t *base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(at), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ inline void to_lds(uint32_t at, const uint8_t *p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(at), "v"(p)
+               : "memory");
+}
+template <int N>
+__device__ inline void wait_loads() {
+  static_assert(N >= 0 && N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+// Products of two tiles of columns with the same tokens, into vector registers:
+// the sums of O take all accumulation registers, and the compiler puts results
+// of its own matrix instructions there.  It does not know what these are, so
+// they bring the waits that the hardware asks for: two cycles after a vector
+// instruction has written an operand, eight before one reads the results
+// (settled()).
+template <int ACT>
+__device__ inline void multiply(f32x4 &x0, f32x4 &x1, const u32x4 &w, const u32x4 &q0,
+                                const u32x4 &q1) {
+  if constexpr (ACT == kBf16)
+    asm("s_nop 1\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %2, %3, %0\n\t"
+        "v_mfma_f32_16x16x32_bf16 %1, %2, %4, %1"
+        : "+v"(x0), "+v"(x1)
+        : "v"(w), "v"(q0), "v"(q1));
+  else
+    asm("s_nop 1\n\t"
+        "v_mfma_f32_16x16x32_f16 %0, %2, %3, %0\n\t"
+        "v_mfma_f32_16x16x32_f16 %1, %2, %4, %1"
+        : "+v"(x0), "+v"(x1)
+        : "v"(w), "v"(q0), "v"(q1));
+}
+__device__ inline void settled(f32x4 &x0, f32x4 &x1) {
+  asm("s_nop 9" : "+v"(x0), "+v"(x1));
+}
+
+// The same for a tile of O whose sums are in vector registers.
+template <int ACT>
+__device__ inline void multiply32(f32x16 &o, const u32x4 &v, const u32x4 &p) {
+  if constexpr (ACT == kBf16)
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
+  else
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
+}
+__device__ inline void settled(f32x16 &o) { asm("s_nop 15" : "+v"(o)); }
+
+// Sums times f, in their accumulation registers.  Rare, so it waits for any
+// matrix instruction before and behind it.
+template <int DT>
+__device__ inline void rescale(f32x16 (&o)[DT], float f) {
+  asm volatile("s_nop 15\n\ts_nop 7" : : : "memory");
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      float t0 = o[dt][i], t1 = o[dt][i + 1], t2 = o[dt][i + 2], t3 = o[dt][i + 3], tmp;
+      asm volatile("v_accvgpr_read_b32 %4, %0\n\tv_mul_f32 %4, %4, %5\n\t"
+                   "v_accvgpr_write_b32 %0, %4\n\t"
+                   "v_accvgpr_read_b32 %4, %1\n\tv_mul_f32 %4, %4, %5\n\t"
+                   "v_accvgpr_write_b32 %1, %4\n\t"
+                   "v_accvgpr_read_b32 %4, %2\n\tv_mul_f32 %4, %4, %5\n\t"
+                   "v_accvgpr_write_b32 %2, %4\n\t"
+                   "v_accvgpr_read_b32 %4, %3\n\tv_mul_f32 %4, %4, %5\n\t"
+                   "v_accvgpr_write_b32 %3, %4"
+                   : "+a"(t0), "+a"(t1), "+a"(t2), "+a"(t3), "=&v"(tmp)
+                   : "v"(f));
+      o[dt][i] = t0;
+      o[dt][i + 1] = t1;
+      o[dt][i + 2] = t2;
+      o[dt][i + 3] = t3;
+    }
+  asm volatile("s_nop 7" : : : "memory");
+}
+
+// Four sums of a tile with something added, likewise.
+__device__ inline void add4(f32x16 &o, int i4, const float (&add)[4]) {
+  float t0 = o[i4 * 4], t1 = o[i4 * 4 + 1], t2 = o[i4 * 4 + 2], t3 = o[i4 * 4 + 3], tmp;
+  asm volatile("v_accvgpr_read_b32 %4, %0\n\tv_add_f32 %4, %4, %5\n\t"
+               "v_accvgpr_write_b32 %0, %4\n\t"
+               "v_accvgpr_read_b32 %4, %1\n\tv_add_f32 %4, %4, %6\n\t"
+               "v_accvgpr_write_b32 %1, %4\n\t"
+               "v_accvgpr_read_b32 %4, %2\n\tv_add_f32 %4, %4, %7\n\t"
+               "v_accvgpr_write_b32 %2, %4\n\t"
+               "v_accvgpr_read_b32 %4, %3\n\tv_add_f32 %4, %4, %8\n\t"
+               "v_accvgpr_write_b32 %3, %4"
+               : "+a"(t0), "+a"(t1), "+a"(t2), "+a"(t3), "=&v"(tmp)
+               : "v"(add[0]), "v"(add[1]), "v"(add[2]), "v"(add[3]));
+  o[i4 * 4] = t0;
+  o[i4 * 4 + 1] = t1;
+  o[i4 * 4 + 2] = t2;
+  o[i4 * 4 + 3] = t3;
+}
+
+struct SeqTiles {
+  Seq q;
+  int32_t units, steps;
+};
+
+// A sequence's units (tiles of its rows times heads) and steps of each.
+template <int QW, int STEP>
+__device__ inline SeqTiles tiles_of(const LatentAttendArgs &a, int s) {
+  SeqTiles w = {{0, 0, 0}, 0, 0};
+  if (s >= a.b.n_seqs) return w;
+  w.q = sequence(a.b, s);
+  if (w.q.rows == 0) return w;
+  w.units = (int32_t)(((int64_t)w.q.rows * a.q_heads + QW * 32 - 1) / (QW * 32));
+  w.steps = max(1, (w.q.len + STEP - 1) / STEP);
+  return w;
+}
+
+template <int ACT, bool FP8, int CT, int QW>
+__global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a) {
+  constexpr int KG = kWaves / QW;        // groups of waves that share tokens
+  constexpr int NT = QW == 4 ? 2 : 1;    // tiles of 16 tokens in a group's step
+  constexpr int STEP = KG * NT * 16;     // tokens of a step
+  static_assert(STEP == latent_step(QW), "the host counts the same steps");
+  constexpr int EB = FP8 ? 1 : 2;
+  constexpr int RC = CT * EB, RR = kTurn * EB;  // bytes of a token's parts in LDS
+  constexpr int TILE = 16 * (RC + RR);
+  constexpr int STAGE = KG * NT * TILE;
+  constexpr int NST = kRing / STAGE < 4 ? kRing / STAGE : 4;  // steps in LDS
+  constexpr int KC = CT * EB / 64, KR = EB;   // 16-byte reads of a tile's keys
+  constexpr int KS = (CT + kTurn) / 32;       // products of a tile's scores
+  constexpr int DT = CT / 32;
+  constexpr int VT = DT == 16 ? 1 : 0;        // tiles of O, the last, in vector registers
+  constexpr int PV = FP8 ? kF16 : ACT;
+  constexpr bool HILO = PV == kBf16 && QW < 4;
+  constexpr float kShift = PV == kF16 ? 7.f : 0.f, kSlack = 8.f;
+  constexpr int LPR = RC / 16, RPI = kLanes / LPR, NI = 8 / RPI;  // loads of 8 tokens' latents
+  constexpr int EIGHTS = NT * 2 / QW;         // eights of tokens that a wave loads in a step
+  constexpr int LOADS = EIGHTS * (NI + 1);
+  static_assert(NST >= 2 && LOADS * (NST - 2) < 64 && EIGHTS >= 1, "shape of the ring");
+  constexpr int CR = CT / 2;                  // elements of a round of the waves' join
+  constexpr int JOIN = KG > 1 ? kWaves * 32 * CR * 4 : 0;
+  constexpr int BYTES = NST * STAGE > JOIN ? NST * STAGE : JOIN;
+  __shared__ __align__(1024) uint8_t ring[BYTES];
+  __shared__ float wave_ml[kWaves][32][2];
+  __shared__ int32_t arrived;
+
+  const KvLayer &kv = a.kv;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, c = lane & 31, h = lane >> 5;
+  const int wave = uniform((int)threadIdx.x >> 6);
+  const int qg = wave % QW, kg = wave / QW;
+  const int HQ = a.q_heads, T = kv.page_tokens, C = a.latent, R = a.turn;
+  const uint32_t row_bytes = (C + R) * EB;
+
+  // ---- this workgroup's unit and part, as many equal parts of a unit as keep
+  // each within `each` steps: the share of a workgroup where all have the
+  // same, or as much more as makes the parts fit the workgroups
+  SeqTiles sw = tiles_of<QW, STEP>(a, lane);
+  int all = sw.units * sw.steps;
+  for (int s0 = kLanes; s0 < a.b.n_seqs; s0 += kLanes) {
+    const SeqTiles w = tiles_of<QW, STEP>(a, s0 + lane);
+    all += w.units * w.steps;
+  }
+  all = __builtin_amdgcn_readlane(scan_wave(all), kLanes - 1);
+  int each = a.least_steps ? max(parts_of_steps(all, a.split_wgs), a.least_steps) : INT32_MAX;
+  for (int i = 0; a.least_steps && a.b.n_seqs <= kLanes; ++i) {
+    const int n = __builtin_amdgcn_readlane(
+        scan_wave(sw.units * parts_of_steps(sw.steps, each)), kLanes - 1);
+    if (n <= a.split_wgs || i == 3) break;
+    each = each + max(1, (int)((float)each * (n - a.split_wgs) / a.split_wgs));
+  }
+  int s = -1, unit = blockIdx.x, parts = 1;
+  Seq sq = {0, 0, 0};
+  int units = 0;
+  for (int s0 = 0; s0 < a.b.n_seqs; s0 += kLanes) {
+    if (s0) sw = tiles_of<QW, STEP>(a, s0 + lane);
+    const int in = parts_of_steps(sw.steps, each);
+    const int upto = scan_wave(sw.units * in);
+    const uint64_t found = __ballot(unit < upto);
+    if (found) {
+      const int l = __builtin_ctzll(found);
+      s = s0 + l;
+      parts = __builtin_amdgcn_readlane(in, l);
+      units = __builtin_amdgcn_readlane(sw.units, l);
+      unit -= __builtin_amdgcn_readlane(upto, l) - units * parts;
+      sq.row0 = __builtin_amdgcn_readlane(sw.q.row0, l);
+      sq.rows = __builtin_amdgcn_readlane(sw.q.rows, l);
+      sq.len = __builtin_amdgcn_readlane(sw.q.len, l);
+      break;
+    }
+    unit -= __builtin_amdgcn_readlane(upto, kLanes - 1);
+  }
+  if (s < 0) return;
+  // tiles that see the most tokens start first
+  const int part = unit % parts, r0 = (units - 1 - unit / parts) * (QW * 32);
+  const int rows_all = sq.rows * HQ, pos0 = sq.len - sq.rows;
+  const int q_first = r0 / HQ, q_last = (min(r0 + QW * 32, rows_all) - 1) / HQ;
+  // rows see at least all_lim tokens, at most `end`
+  const int all_lim = max(min(pos0 + q_first + 1, sq.len), 0);
+  const int end = max(min(pos0 + q_last + 1, sq.len), 0);
+  const int steps = (end + STEP - 1) / STEP, share = steps / parts, more_for = steps % parts;
+  const int from = part * share + min(part, more_for);
+  const int n_steps = share + (part < more_for ? 1 : 0);
+  const int p0 = from * STEP;
+  const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
+  const int last_entry = over_page(kv, max(end - 1, 0));
+
+  // ---- queries: the second operand of S = K Q^T for columns c16 of 16
+  u32x4 qreg[2][KS];
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb) {
+    const int r = r0 + qg * 32 + nb * 16 + c16, qi = r / HQ;
+    const bool there = r < rows_all;
+    const uint16_t *qp = a.q.data + (int64_t)(sq.row0 + (there ? qi : 0)) * a.q.row_stride +
+                         (int64_t)(there ? r - qi * HQ : 0) * a.q.head_stride;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int d = FP8 ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
+      const bool in = d < CT ? d < C : d - CT < R;
+      const uint16_t *p = qp + (d < CT ? d : C + d - CT);
+      if (!there || !in) p = reinterpret_cast<const uint16_t *>(&kZeros);
+      qreg[nb][k] = *reinterpret_cast<const u32x4 *>(p);
+    }
+  }
+  // the row of this lane's column of O^T
+  const int my = r0 + qg * 32 + c, my_q = my / HQ;
+  const bool mine = my < rows_all;
+  const int lim = mine ? min(pos0 + my_q + 1, sq.len) : INT32_MAX;
+
+  // ---- where tokens lie.  A group's tile n is 16 tokens from tile_at(n) on.
+  // Pages of whole tiles: lane l looks up tile n0 + l; else token l % 16 of tile
+  // n0 + l / 16.
+  const bool whole = T % 16 == 0;
+  const int batch = whole ? kLanes : kLanes / 16;
+  auto tile_at = [&](int n) { return p0 + (n / NT * KG + kg) * NT * 16 + n % NT * 16; };
+  auto look = [&](int n0, uint32_t &page, int &slot) {
+    const int tok = whole ? tile_at(n0 + lane) : tile_at(n0 + (lane >> 4)) + c16;
+    const int e = over_page(kv, min(tok, max(end - 1, 0)));
+    const uint32_t pg = table[min(e, last_entry)];
+    slot = max(min(tok, end - 1), 0) - e * T;
+    page = tok < end && pg < (uint32_t)kv.num_pages ? pg : ~0u;
+  };
+
+  // ---- loads.  A token's 16-byte pieces lie in LDS in another order for each
+  // of eight tokens, so that reads of one piece of eight tokens (keys), and of
+  // two pieces of four (values), fall on different banks.
+  auto swap_of = [](int row) { return ((row & 3) << 1) | ((row >> 2) & 1); };
+  const uint32_t ring_at = uniform((uint32_t)(uintptr_t)(lds_u8 *)ring);
+  const bool full = C == CT && R == kTurn;
+  constexpr int TL = RR / 16;  // lanes of a token's turned part
+  // swap_of(i * RPI + lane / LPR) is the two's swaps together: their bits differ
+  const uint32_t lat_row = lane / LPR * row_bytes,
+                 lat_piece = ((lane % LPR) ^ swap_of(lane / LPR)) << 4;
+  const int turn_row = (lane / TL) & 7;
+  const int turn_piece = (lane % TL) ^ (FP8 ? (turn_row >> 1) & 3 : swap_of(turn_row));
+  const uint32_t turn_off = turn_row * row_bytes + C * EB + (turn_piece << 4);
+  uint32_t load_page = ~0u;
+  int load_slot = 0, load_n0 = -(1 << 20);
+  auto load = [&](int step) {
+#pragma unroll
+    for (int e = 0; e < EIGHTS; ++e) {
+      const int eight = qg * EIGHTS + e, kt = eight >> 1, half = (eight & 1) * 8;
+      const int n = step * NT + kt;
+      if (n - load_n0 >= batch) {
+        load_n0 = n - n % batch;
+        look(load_n0, load_page, load_slot);
+      }
+      const int at_n = n - load_n0;
+      const uint32_t tile = ring_at + (step % NST) * STAGE + (kg * NT + kt) * TILE;
+      const uint32_t lat = tile + half * RC, trn = tile + 16 * RC + half * RR;
+      const uint32_t pg = __builtin_amdgcn_readlane(load_page, whole ? at_n : at_n * 16);
+      const int sl = __builtin_amdgcn_readlane(load_slot, whole ? at_n : at_n * 16);
+      if (full && whole && pg != ~0u && tile_at(n) + 16 <= end) {
+        const uint8_t *base = kv.base + ((uint64_t)pg * (uint32_t)kv.piece +
+                                         (uint32_t)(sl + half) * row_bytes);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          to_lds(lat + i * 1024, base + i * RPI * row_bytes,
+                 (lat_piece ^ (swap_of(i * RPI) << 4)) + lat_row);
+        if (!FP8 || lane < 32) to_lds(trn, base, turn_off);
+      } else {  // tokens that nobody attends to, and pieces past a part, are zeros
+#pragma unroll 1
+        for (int i = 0; i <= NI; ++i) {
+          const bool turn = i == NI;
+          const int row = turn ? turn_row : i * RPI + lane / LPR;
+          uint32_t page = pg;
+          int slot = sl + half + row;
+          if (!whole) {
+            page = __shfl(load_page, at_n * 16 + half + row);
+            slot = __shfl(load_slot, at_n * 16 + half + row);
+          }
+          const int piece = turn ? turn_piece : (lane % LPR) ^ swap_of(row);
+          const bool ok = page != ~0u && tile_at(n) + half + row < end &&
+                          piece * 16 < (turn ? R : C) * EB;
+          const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece +
+                                        (uint32_t)slot * row_bytes + (turn ? C * EB : 0) +
+                                        piece * 16);
+          if (!ok) p = reinterpret_cast<const uint8_t *>(&kZeros);
+          if (!FP8 || !turn || lane < 32) to_lds(turn ? trn : lat + i * 1024, p);
+        }
+      }
+    }
+  };
+
+  float m = kNegInf, l = 0.f;
+  f32x16 o[DT - VT], ov[VT + 1];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int dt = 0; dt < DT - VT; ++dt) o[dt][i] = 0.f;
+    if (VT) ov[0][i] = 0.f;
+  }
+  uint32_t odd = 0;
+
+  // places of this lane's reads in a tile
+  int key_at[2], turn_at[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    key_at[i] = c16 * RC + (((i * 4 + g) ^ swap_of(c16)) << 4);
+    turn_at[i] = 16 * RC + c16 * RR +
+                 ((FP8 ? g ^ ((c16 >> 1) & 3) : (i * 4 + g) ^ swap_of(c16)) << 4);
+  }
+  constexpr int VB = FP8 ? 4 : 2;  // 32-element blocks of 128 bytes
+  int val_at[VB][FP8 ? 1 : 2];
+#pragma unroll
+  for (int i = 0; i < VB; ++i) {
+    if constexpr (FP8) {
+      const int row = h * 8 + (c16 >> 1);
+      val_at[i][0] = row * RC + (((i * 2 + (g & 1)) ^ swap_of(row)) << 4) + (c16 & 1) * 8;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = h * 8 + j * 4 + (c16 >> 2), piece = i * 4 + (g & 1) * 2 + ((c16 >> 1) & 1);
+        val_at[i][j] = row * RC + ((piece ^ swap_of(row)) << 4) + (c16 & 1) * 8;
+      }
+    }
+  }
+
+  uint32_t page_of = ~0u;  // of the batch of tiles that is computed
+  float sc_of = 0.f, sr_of = 0.f;
+  int n0_of = -(1 << 20);
+  uint64_t gone_of = 0;
+
+  // Zeros in place of a tile's values that are not finite, once every wave that
+  // shares it has read its keys.
+  auto mend = [&](int step, int kt) {
+    if (QW > 1) __syncthreads();
+    uint8_t *p = ring + (step % NST) * STAGE + (kg * NT + kt) * TILE + qg * (16 / QW) * RC +
+                 lane * 16;
+#pragma unroll 1
+    for (int i = 0; i < 16 / QW * RC / 1024; ++i) {
+      u32x4 v = *reinterpret_cast<u32x4 *>(p + i * 1024);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t bad = odd_mask<ACT, FP8>(v[j]);
+        odd |= bad;
+        v[j] &= ~bad;
+      }
+      *reinterpret_cast<u32x4 *>(p + i * 1024) = v;
+    }
+    if (QW > 1) __syncthreads();
+    else wait_reads();
+  };
+
+  auto compute = [&](int step) {
+    const uint8_t *base = ring + (step % NST) * STAGE + kg * NT * TILE;
+    if (step * NT - n0_of >= batch) {
+      n0_of = step * NT - step * NT % batch;
+      int slot;
+      look(n0_of, page_of, slot);
+      gone_of = __ballot(page_of == ~0u);
+      if (FP8) {
+        const float *sp = kv.scales + (uint64_t)(page_of == ~0u ? 0 : page_of) * 2;
+        sc_of = page_of == ~0u ? 1.f : sp[0];
+        sr_of = page_of == ~0u ? 1.f : sp[1];
+      }
+    }
+    // some row attends to a token here that another does not
+    const int first = p0 + step * STEP;
+    const bool cut = all_lim < end && first + STEP > all_lim;
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt) {
+      const uint8_t *tile = base + kt * TILE;
+      // ---- scores, S^T = K Q^T: columns c16 of two sixteens, tokens g * 4 + i
+      f32x4 x[2], xr[2];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) x[nb] = xr[nb] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KC + KR; ++k) {
+        const bool turn = k >= KC;
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(
+            tile + (turn ? turn_at[(k - KC) & 1] : key_at[k & 1] + (k >> 1) * 128));
+        if constexpr (FP8) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1];
+            const u32x4 af = {fp8_pair<ACT, false>(w0), fp8_pair<ACT, true>(w0),
+                              fp8_pair<ACT, false>(w1), fp8_pair<ACT, true>(w1)};
+            f32x4 *to = turn ? xr : x;
+            multiply<ACT>(to[0], to[1], af, qreg[0][2 * k + j], qreg[1][2 * k + j]);
+          }
+        } else {
+          multiply<ACT>(x[0], x[1], w, qreg[0][k], qreg[1][k]);
+        }
+      }
+      settled(x[0], x[1]);
+      if (FP8) settled(xr[0], xr[1]);
+      // ---- weights.  Exchanged so that a lane has tokens h * 8 + 0 .. 7 of
+      // column c, as the second product takes them
+      const int n = step * NT + kt, at_n = n - n0_of, tok0 = tile_at(n);
+      float y[8], vs[8], sc[4], sr[4];
+      if constexpr (FP8) {
+        if (whole) {
+          const float u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc_of), at_n));
+          const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sr_of), at_n));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) vs[i] = u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[i] = u;
+            sr[i] = v;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[i] = __shfl(sc_of, at_n * 16 + g * 4 + i);
+            sr[i] = __shfl(sr_of, at_n * 16 + g * 4 + i);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) vs[i] = __shfl(sc_of, at_n * 16 + h * 8 + i);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float u = x[0][i], v = x[1][i];
+        if constexpr (FP8) {
+          u = u * sc[i] + xr[0][i] * sr[i];
+          v = v * sc[i] + xr[1][i] * sr[i];
+        }
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v),
+                                                        false, false);
+        y[i] = __uint_as_float(r[0]) * a.scale_log2;
+        y[4 + i] = __uint_as_float(r[1]) * a.scale_log2;
+      }
+      const uint32_t gone = whole ? ((gone_of >> at_n) & 1 ? 0xffffu : 0u)
+                                  : (uint32_t)(gone_of >> (at_n * 16)) & 0xffffu;
+      if (gone || tok0 + 16 > all_lim) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (tok0 + h * 8 + i >= lim || ((gone >> (h * 8 + i)) & 1)) {
+            y[i] = kNegInf;
+            if (FP8) vs[i] = 0.f;
+          }
+      }
+      // the reference counts a value's scale in, within bounds, so that its
+      // weight with the scale fits 16 bits
+      float top = kNegInf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float v = y[i];
+        if constexpr (FP8) v += __log2f(fmaxf(fabsf(vs[i]), 0x1p-60f));
+        top = fmaxf(top, v);
+      }
+      top = max_rows32(top);
+      if (__any(top > m + kSlack)) {
+        const float to = top > m + kSlack ? top : m;
+        const float f = m == kNegInf ? 0.f : exp2_fast(m - to);
+        l *= f;
+        rescale(o, f);
+        if (VT) {
+          settled(ov[0]);
+          ov[0] *= f;
+        }
+        m = to;
+      }
+      const float ref = m == kNegInf ? 0.f : m - kShift;
+      u32x4 ph, pl;
+      {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = exp2_fast(y[i] - ref);
+          l += p[i];
+          if (FP8) p[i] *= vs[i];
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t hi = pack_act<PV>(p[2 * w], p[2 * w + 1]);
+          ph[w] = hi;
+          if constexpr (HILO)
+            pl[w] = pack_act<kBf16>(p[2 * w] - __uint_as_float(hi << 16),
+                                    p[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
+        }
+      }
+      // ---- O^T += V^T P^T.  Where rows attend to different tokens, values that
+      // are not finite count as zero and are left for the end
+      if (cut) mend(step, kt);
+#pragma unroll
+      for (int n = 0; n < DT; ++n) {
+        const int dt = (n + DT - VT) % DT;  // the tile in vector registers first
+        const uint8_t *p = tile + dt / VB * 128;
+        u32x4 af;
+        if constexpr (FP8) {
+          const i32x2 w =
+              __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p + val_at[dt % VB][0]));
+          af = u32x4{fp8_pair<PV, false>(w[0]), fp8_pair<PV, true>(w[0]),
+                     fp8_pair<PV, false>(w[1]), fp8_pair<PV, true>(w[1])};
+        } else {
+          const u32x2 x0 = __builtin_bit_cast(
+              u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][0])));
+          const u32x2 x1 = __builtin_bit_cast(
+              u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][1])));
+          af = u32x4{x0[0], x0[1], x1[0], x1[1]};
+        }
+        if (dt < DT - VT) {
+          f32x16 &to = o[dt < DT - VT ? dt : 0];
+          to = mfma32<PV>(af, ph, to);
+          if constexpr (HILO) to = mfma32<PV>(af, pl, to);
+        } else {
+          multiply32<PV>(ov[0], af, ph);
+          if constexpr (HILO) multiply32<PV>(ov[0], af, pl);
+        }
+      }
+    }
+  };
+
+  // ---- the ring: steps load NST - 1 ahead of their use
+#pragma unroll 1
+  for (int i = 0; i < min(NST - 1, n_steps); ++i) load(i);
+#pragma unroll 1
+  for (int step = 0; step < n_steps; ++step) {
+    const int behind = min(n_steps - 1 - step, NST - 2);  // later steps on their way
+    if (NST > 3 && behind == 2) wait_loads<(NST > 3 ? 2 : 0) * LOADS>();
+    else if (NST > 2 && behind == 1) wait_loads<(NST > 2 ? 1 : 0) * LOADS>();
+    else wait_loads<0>();
+    wait_reads();
+    if (QW > 1) __syncthreads();
+    if (step + NST - 1 < n_steps) load(step + NST - 1);
+    compute(step);
+  }
+
+  if (VT) settled(ov[0]);
+  auto sum_at = [&](int dt, int i) { return dt < DT - VT ? o[dt < DT - VT ? dt : 0][i] : ov[0][i]; };
+
+  // ---- values that are not finite, where not every row attends to them: a
+  // weight that is not zero made the whole row NaN, zero times them is NaN too
+  if (!FP8 && __syncthreads_or(odd != 0)) {
+    asm volatile("s_nop 15\n\ts_nop 7" : : : "memory");  // as in rescale()
+    const int last = min(p0 + n_steps * STEP, end);
+    for (int at = max(all_lim & ~(STEP - 1), p0); at < last; ++at) {
+      const int e = over_page(kv, at);
+      const uint32_t page = table[e];
+      if (page >= (uint32_t)kv.num_pages) continue;
+      const uint16_t *p = reinterpret_cast<const uint16_t *>(
+          kv.base + ((uint64_t)page * (uint32_t)kv.piece + (uint32_t)(at - e * T) * row_bytes));
+      const bool sees = at < lim && (at - p0) / (NT * 16) % KG == kg;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int d = dt * 32 + i4 * 8 + h * 4;
+          const u32x2 w = *reinterpret_cast<const u32x2 *>(p + (d < C ? d : 0));
+          const uint32_t bad[2] = {odd_mask<ACT, false>(w[0]), odd_mask<ACT, false>(w[1])};
+          float add[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            add[i] = d < C && sees && (bad[i >> 1] >> (16 * (i & 1)) & 0xffff)
+                         ? __uint_as_float(0x7fc00000u)
+                         : 0.f;
+          if (dt < DT - VT) {
+            add4(o[dt < DT - VT ? dt : 0], i4, add);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ov[0][i4 * 4 + i] += add[i];
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // a block's loads at a time: registers
+      }
+    }
+  }
+
+  // ---- the groups' sums become one
+  const float total_of = add_rows32(l);
+  const float ref_of = m == kNegInf ? kNegInf : m - kShift;
+  float *part_of = a.parts + (int64_t)blockIdx.x * (QW * 32) * (C + 2);
+  const int64_t row = sq.row0 + my_q, head = my - my_q * HQ;
+  auto emit = [&](int dt, int i4, const f32x4 &v, float norm) {
+    const int d = dt * 32 + i4 * 8 + h * 4;
+    if (!mine || d >= C) return;
+    if (parts == 1) {
+      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride + d) =
+          u32x2{pack_act<ACT>(v[0] * norm, v[1] * norm), pack_act<ACT>(v[2] * norm, v[3] * norm)};
+    } else {
+      float *op = part_of + (qg * 32 + c) * C + d;
+      put_part(op, v[0], v[1]);
+      put_part(op + 2, v[2], v[3]);
+    }
+  };
+  auto emit_statistics = [&](float ref, float total) {
+    if (!mine || h) return;
+    if (parts > 1) put_part(part_of + QW * 32 * C + 2 * (qg * 32 + c), ref, total);
+    else if (a.lse)
+      a.lse[row * HQ + head] =
+          total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+  };
+  if constexpr (KG == 1) {
+    const float norm = total_of == 0.f ? 0.f : 1.f / total_of;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+        emit(dt, i4,
+             f32x4{sum_at(dt, i4 * 4), sum_at(dt, i4 * 4 + 1), sum_at(dt, i4 * 4 + 2),
+                   sum_at(dt, i4 * 4 + 3)},
+             norm);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    emit_statistics(ref_of, total_of);
+  } else {
+    if (h == 0) {
+      wave_ml[wave][c][0] = ref_of;
+      wave_ml[wave][c][1] = total_of;
+    }
+    __syncthreads();  // and the ring has been read
+    float ref = kNegInf, total = 0.f;
+#pragma unroll
+    for (int k = 0; k < KG; ++k) ref = fmaxf(ref, wave_ml[k * QW + qg][c][0]);
+    const float zero = ref == kNegInf ? 0.f : ref;
+#pragma unroll
+    for (int k = 0; k < KG; ++k)
+      total += exp2_fast(wave_ml[k * QW + qg][c][0] - zero) * wave_ml[k * QW + qg][c][1];
+    const float f = ref_of == kNegInf ? 0.f : exp2_fast(ref_of - zero);
+    const float norm = total == 0.f ? 0.f : 1.f / total;
+    constexpr int RD = CR / 32;
+    f32x4 *sums = reinterpret_cast<f32x4 *>(ring);
+#pragma unroll
+    for (int round = 0; round < 2; ++round) {
+      if (round) __syncthreads();
+#pragma unroll
+      for (int d = 0; d < RD; ++d)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int dt = round * RD + d;
+          sums[((wave * RD + d) * 4 + i4) * kLanes + lane] =
+              f32x4{sum_at(dt, i4 * 4) * f, sum_at(dt, i4 * 4 + 1) * f,
+                    sum_at(dt, i4 * 4 + 2) * f, sum_at(dt, i4 * 4 + 3) * f};
+        }
+      __syncthreads();
+      for (int d = kg; d < RD; d += KG)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KG; ++k)
+            v += sums[(((k * QW + qg) * RD + d) * 4 + i4) * kLanes + lane];
+          emit(round * RD + d, i4, v, norm);
+        }
+    }
+    if (kg == 0) emit_statistics(ref, total);
+  }
+  if (parts == 1) return;
+
+  // ---- eight parts are joined by the workgroup of them that ends last, then
+  // eight of those, and so on
+  const int w0 = blockIdx.x - part, rows_here = min(QW * 32, rows_all - r0);
+  for (int stride = 1, level = 0;; stride *= kJoin, ++level) {
+    const int at = part / (stride * kJoin) * (stride * kJoin);  // first of the eight
+    const int of = min((parts - at + stride - 1) / stride, kJoin);
+    const bool last = parts <= stride * kJoin;
+    if (of > 1) {
+      if (!last_of(a.arrivals + w0 + at + level, of, &arrived)) return;
+      // o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, four elements a thread
+      const int quads = C / 4;
+      const int64_t pitch = (int64_t)(QW * 32) * (C + 2);
+      float *p0_of = a.parts + (int64_t)(w0 + at) * pitch;
+      for (int i = threadIdx.x; i < rows_here * quads; i += kThreads) {
+        const int r = i / quads, d = (i - r * quads) * 4;
+        f32x2 ml[kJoin], u[kJoin], v[kJoin];
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+          const float *p = p0_of + min(k, of - 1) * stride * pitch;
+          ml[k] = get_part(p + QW * 32 * C + 2 * r);
+          u[k] = get_part(p + r * C + d);
+          v[k] = get_part(p + r * C + d + 2);
+        }
+        float ref = kNegInf, total = 0.f;
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) ref = fmaxf(ref, ml[k][0]);
+        const float zero = ref == kNegInf ? 0.f : ref;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+          if (k < of) {
+            const float f = exp2_fast(ml[k][0] - zero);
+            total += f * ml[k][1];
+            acc += f * f32x4{u[k][0], u[k][1], v[k][0], v[k][1]};
+          }
+        }
+        if (!last) {
+          // the first part's place: its sums were read above by this thread, its
+          // statistics by others too, so they go behind the last row's
+          put_part(p0_of + r * C + d, acc[0], acc[1]);
+          put_part(p0_of + r * C + d + 2, acc[2], acc[3]);
+        } else {
+          const float f = total == 0.f ? 0.f : 1.f / total;
+          const int rr = r0 + r, q = rr / HQ;
+          *reinterpret_cast<u32x2 *>(a.out.data + (sq.row0 + q) * a.out.row_stride +
+                                     (int64_t)(rr - q * HQ) * a.out.head_stride + d) =
+              u32x2{pack_act<ACT>(acc[0] * f, acc[1] * f), pack_act<ACT>(acc[2] * f, acc[3] * f)};
+          if (a.lse && d == 0)
+            a.lse[(int64_t)(sq.row0 + q) * HQ + rr - q * HQ] =
+                total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+        }
+      }
+      if (!last) {
+        __syncthreads();  // every thread has read the statistics
+        for (int r = threadIdx.x; r < rows_here; r += kThreads) {
+          f32x2 ml[kJoin];
+          float ref = kNegInf, total = 0.f;
+#pragma unroll
+          for (int k = 0; k < kJoin; ++k) {
+            ml[k] = get_part(p0_of + min(k, of - 1) * stride * pitch + QW * 32 * C + 2 * r);
+            ref = fmaxf(ref, ml[k][0]);
+          }
+          const float zero = ref == kNegInf ? 0.f : ref;
+#pragma unroll
+          for (int k = 0; k < kJoin; ++k)
+            if (k < of) total += exp2_fast(ml[k][0] - zero) * ml[k][1];
+          put_part(p0_of + QW * 32 * C + 2 * r, ref, total);
+        }
+      }
+    }
+    if (last) return;
+  }
+}
+
+template <int ACT, bool FP8, int CT>
+hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
+  const dim3 grid((unsigned)a.split_grid), block(kThreads);
+  switch (a.wave_columns) {
+    case 1: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 1>), grid, block, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 2>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 4>), grid, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+template <int ACT, bool FP8>
+hipError_t latents(const LatentAttendArgs &a, hipStream_t s) {
+  if (a.latent <= 256) return columns<ACT, FP8, 256>(a, s);
+  return columns<ACT, FP8, 512>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend_latent(const LatentAttendArgs &a, int act, int fp8, hipStream_t s) {
+  (void)hipGetLastError();
+  if (act == kBf16) return fp8 ? latents<kBf16, true>(a, s) : latents<kBf16, false>(a, s);
+  return fp8 ? latents<kF16, true>(a, s) : latents<kF16, false>(a, s);
+}
+
+}  // namespace ea

@@ -92,6 +92,26 @@ struct SelectArgs {
   int32_t blocks_wave;      // blocks one wave scores
 };
 
+// A cache of latents is a KvLayer of one head of half a token's row: a token
+// has `latent` elements, then `turn` ones, in place of a key and a value; the
+// scales of a block are those of the two parts.
+struct LatentAttendArgs {
+  KvLayer kv;
+  BatchRows b;
+  HeadRows q, out;          // [n_rows][q_heads][latent + turn], [n_rows][q_heads][latent]
+  float *lse;               // [n_rows][q_heads] or nullptr
+  int32_t latent, turn;
+  int32_t q_heads;
+  float scale_log2;         // softmax scale times log2(e)
+  // A workgroup takes 32 * wave_columns (1, 2, 4) rows times heads of a
+  // sequence, a unit; split_wgs, least_steps, split_grid, parts and arrivals are
+  // as for the split kernel.
+  int32_t wave_columns;
+  int32_t split_wgs, least_steps, split_grid;
+  float *parts;             // [split_grid][32 * wave_columns][latent + 2]
+  int32_t *arrivals;
+};
+
 // Parts of at most `each` steps that `steps` steps come in.  No sum of the two,
 // which could pass 32 bits.
 constexpr int32_t parts_of_steps(int32_t steps, int32_t each) {
@@ -111,11 +131,15 @@ constexpr int32_t split_resident(int32_t head_dim, int32_t columns) {
   return head_dim <= 64 && columns <= 16 ? 2 : 1;
 }
 
+// Tokens of a step of the latent kernel with this many groups of 32 columns.
+constexpr int32_t latent_step(int32_t wave_columns) { return wave_columns == 1 ? 64 : 32; }
+
 // Counters at the start of an attention workspace: a unit's parts done.  More
 // units than kSplitUnits are not split.
 constexpr int32_t kSplitUnits = 4096, kArrivals = 8192;
 
 constexpr int32_t kMaxHeadDim = 256;
+constexpr int32_t kMaxLatent = 512, kMaxTurn = 64;
 constexpr int32_t kMaxSelectBlocks = 65536;
 
 // Most query rows times heads of a group that the split kernel takes (its
@@ -133,6 +157,7 @@ hipError_t launch_bounds(const KvLayer &kv, int act, int fp8, int32_t layers, in
 hipError_t launch_attend_split(const AttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_attend_chunk(const AttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs &a, int act, hipStream_t s);
+hipError_t launch_attend_latent(const LatentAttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_select(const SelectArgs &a, int act, hipStream_t s);
 
 }  // namespace ea

@@ -1,0 +1,117 @@
+// Entry points of the latent cache (include/ea.h): validation, the split of an
+// attention call along the tokens, and the launches.  They allocate nothing.
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+#include "ea.h"
+#include "ea_internal.hpp"
+#include "ea_kv_host.hpp"
+#include "ea_kv_ops.hpp"
+
+using namespace ea::host;
+
+namespace {
+
+int check_latents(const ea_cache *c, int32_t latent, int32_t turn, int32_t dtype) {
+  if (!c || (dtype != EA_BF16 && dtype != EA_F16)) return EA_EINVAL;
+  const ea_cache_desc &d = ea::cache_desc(c);
+  if (latent < 1 || turn < 1 || d.num_kv_heads != 1 || (int64_t)latent + turn != 2LL * d.head_dim)
+    return EA_EINVAL;
+  if (d.elem_bytes != 1 && d.elem_bytes != 2) return EA_ENOTSUP;
+  if (latent % 16 != 0 || latent > ea::kMaxLatent || turn % 16 != 0 || turn > ea::kMaxTurn)
+    return EA_ENOTSUP;
+  if ((int64_t)d.num_pages * d.page_tokens > INT32_MAX) return EA_ENOTSUP;
+  // places inside a page are 32 bits
+  if (2LL * d.page_tokens * d.head_dim * d.elem_bytes > (1 << 30)) return EA_ENOTSUP;
+  return EA_OK;
+}
+
+// How an attention call is split along its tokens, and its workspace: the
+// counters, always first, then the parts.
+constexpr int64_t kCounters = ea::kArrivals * 4;
+struct Parts {
+  int32_t wave_columns, wgs, least_steps, grid;
+  int64_t bytes;
+};
+
+Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *a) {
+  Parts p{};
+  const int64_t most = (int64_t)b->max_rows * a->q_heads;
+  p.wgs = std::min(compute_units(ea::cache_device(c)), ea::kArrivals - ea::kSplitUnits);
+  p.wave_columns = most <= 32 ? 1 : most <= 64 ? 2 : 4;
+  const int64_t tile = 32 * p.wave_columns;
+  const int64_t units =
+      std::min<int64_t>(b->n_seqs * ((most + tile - 1) / tile),
+                        (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
+  p.least_steps = units <= ea::kSplitUnits ? 2 : 0;
+  const int64_t step = ea::latent_step(p.wave_columns);
+  const int64_t steps = (b->max_kv + step - 1) / step;
+  const int64_t whole = p.least_steps ? (steps + p.least_steps - 1) / p.least_steps : 1;
+  p.grid = (int32_t)std::min<int64_t>(p.wgs + units, units * whole);
+  if (p.grid > units) p.bytes = kCounters + up((int64_t)p.grid * tile * (a->latent_dim + 2) * 4, 16);
+  return p;
+}
+
+int check_attention(const ea_cache *c, const ea_batch *b, const ea_latent_attention *a) {
+  if (!a) return EA_EINVAL;
+  KV_TRY(check_latents(c, a->latent_dim, a->rope_dim, a->dtype));
+  KV_TRY(check_batch(ea::cache_desc(c), b));
+  if (a->q_heads < 1) return EA_EINVAL;
+  if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return EA_EINVAL;
+  if (empty(b)) return EA_OK;
+  // rows times heads, and steps of all units, are counted in 32 bits
+  const int64_t most = (int64_t)b->max_rows * a->q_heads;
+  if ((int64_t)b->n_rows * a->q_heads > INT32_MAX / 4 || most > INT32_MAX / 4) return EA_ENOTSUP;
+  if ((int64_t)b->n_seqs * (most / 32 + 1) > INT32_MAX / (b->max_kv / 32 + 1)) return EA_ENOTSUP;
+  return EA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t ea_attend_latent_workspace(const ea_cache *c, const ea_batch *b,
+                                   const ea_latent_attention *a) {
+  KV_TRY(check_attention(c, b, a));
+  if (empty(b)) return 0;
+  return parts_of(c, b, a).bytes;
+}
+
+int ea_attend_latent(ea_cache *c, int32_t layer, const ea_batch *b, const ea_latent_attention *a,
+                     void *workspace, int64_t workspace_bytes, hipStream_t stream) {
+  KV_TRY(check_attention(c, b, a));
+  ea::LatentAttendArgs k{};
+  KV_TRY(layer_of(c, nullptr, layer, &k.kv));
+  if (empty(b)) return EA_OK;
+  KV_TRY(check_rows(a->q));
+  KV_TRY(check_rows(a->out));
+  if (a->lse && !aligned(a->lse, 4)) return EA_EINVAL;
+  const Parts p = parts_of(c, b, a);
+  if (workspace_bytes < p.bytes || (p.bytes > 0 && (!workspace || !aligned(workspace, 16))))
+    return EA_EINVAL;
+  k.b = batch_rows(b);
+  k.q = rows(a->q);
+  k.out = rows(a->out);
+  k.lse = a->lse;
+  k.latent = a->latent_dim;
+  k.turn = a->rope_dim;
+  k.q_heads = a->q_heads;
+  k.scale_log2 = a->scale * 1.4426950408889634f;
+  k.wave_columns = p.wave_columns;
+  k.split_wgs = p.wgs;
+  k.least_steps = p.least_steps;
+  k.split_grid = p.grid;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  k.arrivals = reinterpret_cast<int32_t *>(ws);
+  k.parts = reinterpret_cast<float *>(ws + kCounters);
+  OnDevice on(ea::cache_device(c));
+  KV_HIP(on.status());
+  KV_HIP(ea::launch_attend_latent(k, a->dtype, ea::cache_desc(c).elem_bytes == 1, stream));
+  return EA_OK;
+}
+
+}  // extern "C"
