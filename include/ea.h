@@ -722,6 +722,29 @@ int ea_select_blocks(ea_cache *cache, const ea_cache_planes *planes, int32_t lay
  * operators. */
 
 typedef struct {
+  ea_rows latent;      /* [n_rows][1][latent_dim]: as they are cached         */
+  ea_rows key;         /* [n_rows][1][rope_dim]: the part that turns          */
+  ea_rows q, q_out;    /* [n_rows][q_heads][rope_dim]: the queries' parts that
+                          turn; q.data NULL: no queries.  q_out may be q      */
+  const float *rope;   /* float32 [rope_len][rope_dim], 16-byte aligned, as for
+                          ea_append; NULL: parts stay as they are             */
+  int32_t rope_len;    /* >= max_kv                                           */
+  int32_t latent_dim, rope_dim;
+  int32_t interleaved; /* pairs (2i, 2i+1) instead of (i, i + rope_dim/2)     */
+  int32_t q_heads;
+  int32_t dtype;       /* ea_dtype of latent, key, q, q_out                   */
+} ea_latent_append;
+
+/* Append a step's tokens to layer `layer`, as ea_append_kv does keys and
+ * values: row r of sequence s goes to position kv_len[s] - rows + r, its latent
+ * as it is, its key part rotated in 32 bits and rounded once; q_out gets the
+ * rotated parts of the queries.  fp8: the scales of a block's latents and of
+ * its key parts follow ea_append_kv's rule.  Pages that get new tokens must
+ * belong to one sequence of the batch alone. */
+int ea_append_latent(ea_cache *cache, int32_t layer, const ea_batch *batch,
+                     const ea_latent_append *args, hipStream_t stream);
+
+typedef struct {
   ea_rows q;           /* [n_rows][q_heads][latent_dim + rope_dim]: a head's
                           query against latents (its part before rotation times
                           the head's key weights), then its rotated part      */
@@ -751,6 +774,62 @@ int64_t ea_attend_latent_workspace(const ea_cache *cache, const ea_batch *batch,
 int ea_attend_latent(ea_cache *cache, int32_t layer, const ea_batch *batch,
                      const ea_latent_attention *args, void *workspace,
                      int64_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------- pages of a cache
+ *
+ * What a fork or an edit of a context does to its pages (not in the paper).
+ * Page lists, tables and positions are device memory, the calls allocate
+ * nothing and are asynchronous on `stream`; what lies outside the bounds given
+ * is skipped as said, and reads and writes nothing outside the cache.
+ *
+ * Copy pages d_src[i] to d_dst[i], i < n (device int32), in every layer, with
+ * the cache's scales and the planes given: the block that a forked context
+ * goes on writing, pages that a pool draws together.  Pairs with an id outside
+ * the cache are skipped.  No page may be written twice, or read by one pair
+ * and written by another.  Any cache. */
+int ea_copy_pages(ea_cache *cache, const ea_cache_planes *planes, const int32_t *d_src,
+                  const int32_t *d_dst, int32_t n, hipStream_t stream);
+
+typedef struct {
+  const int32_t *src_table;   /* int32[n_seqs][src_stride]: pages now         */
+  const int32_t *dst_table;   /* int32[n_seqs][dst_stride]: pages to fill     */
+  int64_t src_stride;         /* * page_tokens >= max_kv                      */
+  int64_t dst_stride;         /* * page_tokens >= max_tokens                  */
+  const int32_t *tokens;      /* int32[n_tokens]: positions of kept tokens    */
+  const int32_t *token_start; /* int32[n_seqs+1], non-decreasing: a sequence's
+                                 tokens are token_start[s] .. [s+1]-1         */
+  const int32_t *dst_first;   /* int32[n_seqs]: new position of a sequence's
+                                 first kept token; NULL: 0                    */
+  const float *rope;          /* float32 [rope_len][rope_dim], 16-byte aligned:
+                                 cosines and sines as for ea_append; NULL: keys
+                                 stay as they are                             */
+  int32_t rope_len;           /* more than any token moves                    */
+  int32_t rope_dim;           /* as for ea_append; of a latent cache its own  */
+  int32_t interleaved;
+  int32_t latent_dim;         /* > 0: a latent cache; 0: keys and values      */
+  int32_t n_seqs;
+  int32_t n_tokens;           /* most tokens of all sequences                 */
+  int32_t max_tokens;         /* most tokens of one sequence                  */
+  int32_t max_kv;             /* positions in tokens are below this           */
+  int32_t dtype;              /* ea_dtype of a 16-bit cache                   */
+  int32_t _pad;
+} ea_move;
+
+/* Move kept tokens of sequences together in layers [layer_begin, layer_begin +
+ * layer_count): token i of sequence s, now at position p = tokens[..] of
+ * src_table, goes to slot i mod T of page dst_table[s*dst_stride + i/T] and to
+ * position dst_first[s] + i.  Its key turns by the difference of the
+ * positions, in 32 bits and rounded once (the angles of a position must be its
+ * multiples of those of position 1: what scales cosines and sines belongs into
+ * the softmax scale); a key that stays in its position, and values, keep their
+ * value.  fp8 blocks get the scales that ea_append_kv gives a new block, which
+ * requantises; with bounds, the blocks' bounds are made from their keys.  A
+ * token whose position or page is outside the bounds, or that moves by
+ * rope_len or more, becomes zeros.  Slots behind the last token stay as they
+ * are.  The pages written must belong to one sequence alone and not be read
+ * by the call; pages read may be shared. */
+int ea_move_tokens(ea_cache *cache, const ea_cache_planes *planes, int32_t layer_begin,
+                   int32_t layer_count, const ea_move *args, hipStream_t stream);
 
 /* How stores and loads cross the host link:
  *  EA_PLAN_DIRECT: one kernel reads/writes the mapped pinned slots;

@@ -104,6 +104,22 @@ class Selection(C.Structure):
                 ("dtype", C.c_int32), ("_pad", C.c_int32)]
 
 
+class LatentAppend(C.Structure):
+    _fields_ = [("latent", Rows), ("key", Rows), ("q", Rows), ("q_out", Rows),
+                ("rope", C.c_void_p), ("rope_len", C.c_int32), ("latent_dim", C.c_int32),
+                ("rope_dim", C.c_int32), ("interleaved", C.c_int32), ("q_heads", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class Move(C.Structure):
+    _fields_ = [("src_table", C.c_void_p), ("dst_table", C.c_void_p), ("src_stride", C.c_int64),
+                ("dst_stride", C.c_int64), ("tokens", C.c_void_p), ("token_start", C.c_void_p),
+                ("dst_first", C.c_void_p), ("rope", C.c_void_p), ("rope_len", C.c_int32),
+                ("rope_dim", C.c_int32), ("interleaved", C.c_int32), ("latent_dim", C.c_int32),
+                ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_tokens", C.c_int32),
+                ("max_kv", C.c_int32), ("dtype", C.c_int32), ("_pad", C.c_int32)]
+
+
 class LatentAttention(C.Structure):
     _fields_ = [("q", Rows), ("out", Rows), ("lse", C.c_void_p), ("latent_dim", C.c_int32),
                 ("rope_dim", C.c_int32), ("q_heads", C.c_int32), ("dtype", C.c_int32),
@@ -159,6 +175,9 @@ SIGNATURES = {
     "ea_attend": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
     "ea_select_workspace": (_I64, [_P, _P, _P]),
     "ea_select_blocks": (_INT, [_P, _P, _I32, _P, _P, _P, _I64, _P]),
+    "ea_append_latent": (_INT, [_P, _I32, _P, _P, _P]),
+    "ea_copy_pages": (_INT, [_P, _P, _P, _P, _I32, _P]),
+    "ea_move_tokens": (_INT, [_P, _P, _I32, _I32, _P, _P]),
     "ea_attend_latent_workspace": (_I64, [_P, _P, _P]),
     "ea_attend_latent": (_INT, [_P, _I32, _P, _P, _P, _I64, _P]),
     "ea_tier_set_plan": (_INT, [_P, _INT, _INT]),

@@ -169,6 +169,12 @@ class Cache:
             raise ValueError(f"{what} must have the dtype of the call's other rows")
         return t.data_ptr(), stride[0], stride[1]
 
+    def _rope(self, rope):
+        if rope.device != self._device or rope.dtype not in _f32() or rope.dim() != 2 or \
+                not rope.is_contiguous():
+            raise ValueError("rope must be a contiguous float32 matrix on the cache's device")
+        return (rope.data_ptr(), *rope.shape)
+
     def _stream(self, s):
         return _current_raw(self._device.index) if s is None else _stream(s)
 
@@ -188,10 +194,7 @@ class Cache:
             a.q = self._rows(q, "q", n, heads, act)
             a.q_out = self._rows(q_out, "q_out", n, heads, act)
         if rope is not None:
-            if rope.device != self._device or rope.dtype not in _f32() or rope.dim() != 2 or \
-                    not rope.is_contiguous():
-                raise ValueError("rope must be a contiguous float32 matrix on the cache's device")
-            a.rope, (a.rope_len, a.rope_dim) = rope.data_ptr(), rope.shape
+            a.rope, a.rope_len, a.rope_dim = self._rope(rope)
         a.interleaved, a.dtype = interleaved, act
         N.check("ea_append_kv", self._lib.ea_append_kv(
             self._h, self._planes_ref, layer, batch.ref, C.byref(a), self._stream(stream)))
@@ -230,6 +233,69 @@ class Cache:
         N.check("ea_attend", self._lib.ea_attend(
             self._h, self._planes_ref, layer, batch.ref, ref,
             None if ws is None else ws.data_ptr(), need, s))
+
+    def copy_pages(self, src, dst, stream=None):
+        """Pages src[i] copied to dst[i] (int32 device tensors) in every layer,
+        with their scales and planes: the block that a forked context goes on
+        writing, or pages that a pool draws together.  No page may be written
+        twice, or read by one pair and written by another."""
+        _device_ints(src, "src", self._device)
+        _device_ints(dst, "dst", self._device)
+        if src.numel() != dst.numel():
+            raise ValueError(f"{src.numel()} pages to read, {dst.numel()} to write")
+        N.check("ea_copy_pages", self._lib.ea_copy_pages(
+            self._h, self._planes_ref, src.data_ptr(), dst.data_ptr(), src.numel(),
+            self._stream(stream)))
+
+    def move_tokens(self, src_table, dst_table, tokens, token_start, max_tokens, max_kv,
+                    dst_first=None, rope=None, interleaved=False, layer_begin=0, layer_count=None,
+                    dtype=None, stream=None):
+        """Kept tokens of edited contexts moved together into other pages:
+        those of sequence s, tokens[token_start[s] .. token_start[s + 1]) by
+        their positions in src_table's pages, fill the pages of dst_table's row
+        in order, from position dst_first[s] (0 if None) on, keys turned by the
+        difference of the positions where `rope` (as for append_kv) is given.
+        All arrays int32 device tensors; max_tokens and max_kv bound a
+        sequence's kept tokens and the positions.  dtype: of a 16-bit cache
+        (torch.bfloat16 if None)."""
+        for t, what in ((src_table, "src_table"), (dst_table, "dst_table")):
+            if t.device != self._device or str(t.dtype) != "torch.int32" or t.dim() != 2 or \
+                    (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError(f"{what} must be an int32 matrix with contiguous rows on the "
+                                 "cache's device")
+        n = src_table.shape[0]
+        _device_ints(tokens, "tokens", self._device)
+        _device_ints(token_start, "token_start", self._device)
+        if dst_table.shape[0] != n or token_start.numel() != n + 1:
+            raise ValueError("dst_table needs a row, token_start an entry (and one more), for "
+                             "each row of src_table")
+        if max_kv > src_table.shape[1] * self.page_tokens or \
+                max_tokens > dst_table.shape[1] * self.page_tokens:
+            raise ValueError(f"tables of {src_table.shape[1]} and {dst_table.shape[1]} pages of "
+                             f"{self.page_tokens} tokens, max_kv {max_kv}, max_tokens {max_tokens}")
+        a = N.Move(src_table.data_ptr(), dst_table.data_ptr(),
+                   src_table.stride(0) if n > 1 else src_table.shape[1],
+                   dst_table.stride(0) if n > 1 else dst_table.shape[1],
+                   tokens.data_ptr(), token_start.data_ptr())
+        if dst_first is not None:
+            _device_ints(dst_first, "dst_first", self._device)
+            if dst_first.numel() != n:
+                raise ValueError("dst_first needs one position for each row of src_table")
+            a.dst_first = dst_first.data_ptr()
+        a.rope_dim, a.latent_dim = self._moved
+        if rope is not None:
+            a.rope, a.rope_len, dim = self._rope(rope)
+            if a.latent_dim and dim != a.rope_dim:
+                raise ValueError(f"rope must have {a.rope_dim} columns")
+            a.rope_dim = dim
+        a.interleaved, a.n_seqs, a.n_tokens = interleaved, n, tokens.numel()
+        a.max_tokens, a.max_kv = max_tokens, max_kv
+        a.dtype = N.EA_BF16 if dtype is None else _act(dtype)
+        count = self.num_layers - layer_begin if layer_count is None else layer_count
+        N.check("ea_move_tokens", self._lib.ea_move_tokens(
+            self._h, self._planes_ref, layer_begin, count, C.byref(a), self._stream(stream)))
+
+    _moved = (0, 0)  # rope_dim and latent_dim of a cache of latents
 
     def _lse(self, lse, n, heads):
         if lse.device != self._device or lse.dtype not in _f32() or \
@@ -277,12 +343,39 @@ class LatentCache(Cache):
                          elem_bytes, scales=scales)
         self.latent_dim, self.rope_dim = latent_dim, rope_dim
         self._shape = ("latent", latent_dim, rope_dim, page_tokens, elem_bytes)
+        self._moved = (rope_dim, latent_dim)
 
     def _keys_and_values(self, *args, **kwargs):
         raise TypeError("a cache of latents holds no keys and values: append_latent and "
                         "attend_latent are its operators")
 
     append_kv = attend = select_blocks = bound_blocks = _keys_and_values
+
+    def append_latent(self, layer, batch, latent, key, rope=None, q=None, q_out=None,
+                      interleaved=False, stream=None):
+        """Append a step's tokens: latent [n_rows, 1, latent_dim] and key
+        [n_rows, 1, rope_dim] (any row stride) go to the last positions of their
+        sequences, key parts rotated by `rope` (float32 [positions, rope_dim],
+        cosines then sines); q_out gets q [n_rows, q_heads, rope_dim] rotated
+        (it may be q)."""
+        self._fits(batch)
+        act, n = _dtype(latent), batch.n_rows
+        a = N.LatentAppend(self._rows(latent, "latent", n, 1, act, self.latent_dim),
+                           self._rows(key, "key", n, 1, act, self.rope_dim))
+        if q is not None:
+            if q_out is None:
+                raise ValueError("q needs a q_out")
+            a.q_heads = heads = q.shape[1]
+            a.q = self._rows(q, "q", n, heads, act, self.rope_dim)
+            a.q_out = self._rows(q_out, "q_out", n, heads, act, self.rope_dim)
+        if rope is not None:
+            a.rope, a.rope_len, dim = self._rope(rope)
+            if dim != self.rope_dim:
+                raise ValueError(f"rope must have {self.rope_dim} columns")
+        a.latent_dim, a.rope_dim = self.latent_dim, self.rope_dim
+        a.interleaved, a.dtype = interleaved, act
+        N.check("ea_append_latent", self._lib.ea_append_latent(
+            self._h, layer, batch.ref, C.byref(a), self._stream(stream)))
 
     def attend_latent(self, layer, batch, q, out, scale, lse=None, stream=None):
         """Attention of absorbed queries q [n_rows, q_heads, latent_dim +

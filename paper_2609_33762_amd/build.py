@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libea.so")
 SOURCES = ["ea_copy_kernels.hip", "ea_sha256_kernels.hip", "ea_tier_meta.cpp",
            "ea_api.cpp", "ea_hash.cpp", "ea_stack.cpp", "ea_controller.cpp",
            "ea_attend_split.hip", "ea_attend_chunk.hip", "ea_select_kernels.hip",
-           "ea_append_kernels.hip", "ea_attend_latent.hip", "ea_kv_ops.cpp", "ea_latent_ops.cpp"]
+           "ea_append_kernels.hip", "ea_attend_latent.hip", "ea_latent_append.hip",
+           "ea_page_kernels.hip", "ea_kv_ops.cpp", "ea_latent_ops.cpp", "ea_page_ops.cpp"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,159 @@
+// What the kernels that write blocks of a cache share: a lane's place in a
+// token's head, stored values, fp8 codes, a block's bounds.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "ea_kv_device.hpp"
+
+namespace ea {
+
+// Lanes side by side on one token's head, two pieces of 8 elements each.
+constexpr int lanes_of(int head_dim) { return head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
+
+template <int ACT>
+__device__ inline void read8(const uint16_t *p, float x[8]) {
+  const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = act_to_float<ACT>((uint16_t)(v[i >> 1] >> (16 * (i & 1))));
+}
+
+// What a lane has of every head: elements d[0] ..+7 and d[1] ..+7, and whether
+// the head has them.  Rotation pairs i with i + dim / 2: where that is whole
+// pieces, a lane has both halves of its pairs.
+struct Place {
+  int d[2];
+  bool in[2];
+  bool paired;  // its two pieces turn together
+};
+__device__ inline Place place_of(int lp, int D, bool turn, int dim, bool interleaved) {
+  Place p;
+  const int half = dim >> 1;
+  const bool halves = turn && !interleaved && (half & 7) == 0;
+  p.paired = halves && lp * 8 < half;
+  if (p.paired) {
+    p.d[0] = lp * 8;
+    p.d[1] = lp * 8 + half;
+  } else {  // neighbours: of what does not turn, or of the whole head
+    p.d[0] = halves ? dim + (lp * 8 - half) * 2 : lp * 16;
+    p.d[1] = p.d[0] + 8;
+  }
+  p.in[0] = p.d[0] < D;
+  p.in[1] = p.d[1] < D;
+  return p;
+}
+
+// Largest value over the lanes with the same place in groups of LP.
+template <int LP>
+__device__ inline float max_tokens(float v) {
+  if constexpr (LP <= 4) v = fmaxf(v, row_ror<0x124>(v));
+  if constexpr (LP <= 8) v = fmaxf(v, row_ror<0x128>(v));
+  return max_rows16(v);
+}
+
+// Four fp8 codes from four values and back.
+__device__ inline uint32_t fp8_word(float a, float b, float c, float d) {
+  uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+__device__ inline void fp8_values(uint32_t w, float x[4]) {
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+  const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  x[0] = a[0];
+  x[1] = a[1];
+  x[2] = b[0];
+  x[3] = b[1];
+}
+
+// Elements d0 .. d0+7 of a stored token as values.
+template <int ACT, bool FP8>
+__device__ inline void stored8(const uint8_t *p, float scale, float x[8]) {
+  if constexpr (FP8) {
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    fp8_values(w[0], x);
+    fp8_values(w[1], x + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= scale;
+  } else {
+    read8<ACT>(reinterpret_cast<const uint16_t *>(p), x);
+  }
+}
+
+// Bounds of a block's keys as whole numbers: lowest rounded down, highest
+// rounded up, in units of a power of two that holds them within 127.  LP lanes
+// hold a token's head; every (64 / LP)-th token is a lane's.  Values that are
+// not finite do not set the unit; an infinity is the largest whole number.
+template <int LP>
+__device__ inline void write_bounds(const KvLayer &kv, int page, int h, int lane, const Place &p,
+                                    float lo[16], float hi[16]) {
+  const int D = kv.head_dim;
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    lo[i] = -max_tokens<LP>(-lo[i]);
+    hi[i] = max_tokens<LP>(hi[i]);
+    if (p.in[i >> 3] && finite(lo[i])) amax = fmaxf(amax, fabsf(lo[i]));
+    if (p.in[i >> 3] && finite(hi[i])) amax = fmaxf(amax, fabsf(hi[i]));
+  }
+  const float s = int8_scale(max_wave(amax)), inv = power_inverse(s);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    if (lane >= LP || !p.in[n]) continue;
+    u32x2 wl = {0, 0}, wh = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int l = (int)fmaxf(fminf(floorf(lo[n * 8 + i] * inv), 127.f), -127.f);
+      const int u = (int)fmaxf(fminf(ceilf(hi[n * 8 + i] * inv), 127.f), -127.f);
+      wl[i >> 2] |= (uint32_t)(uint8_t)l << (8 * (i & 3));
+      wh[i >> 2] |= (uint32_t)(uint8_t)u << (8 * (i & 3));
+    }
+    int8_t *q = kv.bounds + ((int64_t)page * 2 * kv.heads + h) * D + p.d[n];
+    *reinterpret_cast<u32x2 *>(q) = wl;
+    *reinterpret_cast<u32x2 *>(q + (int64_t)kv.heads * D) = wh;
+  }
+  if (lane == 0) kv.bound_scales[(int64_t)page * kv.heads + h] = s;
+}
+
+// Block j of a sequence's moved tokens: its page, n tokens from list place `at`
+// on, their first new position.  n 0: nothing to write.
+struct MovedBlock {
+  int32_t page, n, at;
+  int64_t pos;
+  const int32_t *table;  // of the old pages
+};
+__device__ inline MovedBlock moved_block(const MoveArgs &a, int s, int j) {
+  MovedBlock m = {-1, 0, 0, 0, a.src_table + (int64_t)s * a.src_stride};
+  const int T = a.kv.page_tokens;
+  const int lo = min(max(a.token_start[s], 0), a.n_tokens);
+  const int hi = min(max(a.token_start[s + 1], lo), a.n_tokens);
+  const int first = j * T, n = min(min(hi - lo, a.max_tokens) - first, T);
+  if (n <= 0) return m;
+  const int page = a.dst_table[(int64_t)s * a.dst_stride + j];
+  if ((uint32_t)page >= (uint32_t)a.kv.num_pages) return m;
+  m.page = page;
+  m.n = n;
+  m.at = lo + first;
+  m.pos = (int64_t)(a.dst_first ? a.dst_first[s] : 0) + first;
+  return m;
+}
+
+// Where token i of the block was, and how far it moves.  page -1: nowhere.
+struct MovedToken {
+  int32_t page, slot, by;
+};
+__device__ inline MovedToken moved_token(const MoveArgs &a, const MovedBlock &m, int i) {
+  MovedToken t = {-1, 0, 0};
+  const int old = a.tokens[m.at + i];
+  if ((uint32_t)old >= (uint32_t)a.max_kv) return t;
+  const int e = over_page(a.kv, old);
+  const int64_t by = m.pos + i - old;
+  const int page = m.table[e];
+  if ((uint32_t)page >= (uint32_t)a.kv.num_pages) return t;
+  if (a.rope && (by >= a.rope_len || by <= -(int64_t)a.rope_len)) return t;
+  t.page = page;
+  t.slot = old - e * a.kv.page_tokens;
+  t.by = a.rope ? (int32_t)by : 0;
+  return t;
+}
+
+}  // namespace ea

@@ -106,6 +106,21 @@ inline int check_cache(const ea_cache *c, int32_t dtype) {
   return EA_OK;
 }
 
+// A cache of latents: a token's row in place of one head's key and value.
+inline int check_latents(const ea_cache *c, int32_t latent, int32_t turn, int32_t dtype) {
+  if (!c || (dtype != EA_BF16 && dtype != EA_F16)) return EA_EINVAL;
+  const ea_cache_desc &d = ea::cache_desc(c);
+  if (latent < 1 || turn < 1 || d.num_kv_heads != 1 || (int64_t)latent + turn != 2LL * d.head_dim)
+    return EA_EINVAL;
+  if (d.elem_bytes != 1 && d.elem_bytes != 2) return EA_ENOTSUP;
+  if (latent % 16 != 0 || latent > ea::kMaxLatent || turn % 16 != 0 || turn > ea::kMaxTurn)
+    return EA_ENOTSUP;
+  if ((int64_t)d.num_pages * d.page_tokens > INT32_MAX) return EA_ENOTSUP;
+  // places inside a page are 32 bits
+  if (2LL * d.page_tokens * d.head_dim * d.elem_bytes > (1 << 30)) return EA_ENOTSUP;
+  return EA_OK;
+}
+
 // The layer with its planes.  Scales: of a block and head, or the cache's
 // own one for a block.
 inline int layer_of(const ea_cache *c, const ea_cache_planes *planes, int32_t layer,

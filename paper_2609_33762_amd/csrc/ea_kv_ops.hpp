@@ -112,6 +112,46 @@ struct LatentAttendArgs {
   int32_t *arrivals;
 };
 
+struct LatentAppendArgs {
+  KvLayer kv;
+  BatchRows b;
+  HeadRows latents, key;    // [n_rows][1][latent], [n_rows][1][turn]
+  HeadRows q, q_out;        // [n_rows][q_heads][turn]; q.data null: no queries
+  const float *rope;        // [rope_len][turn]: cosines, then sines; or nullptr
+  int32_t latent, turn;
+  int32_t interleaved;
+  int32_t q_heads;
+  int32_t pages_most;       // pages one sequence's new tokens can touch
+};
+
+// Kept tokens of sequences on their way to other pages, in `layers` layers from
+// kv's on.  Keys and values, or (latent > 0) rows of a latent cache.
+struct MoveArgs {
+  KvLayer kv;
+  int64_t layer_bytes, layer_scales;  // from layer to layer
+  const int32_t *src_table, *dst_table;
+  int64_t src_stride, dst_stride;
+  const int32_t *tokens;        // [n_tokens] old positions
+  const int32_t *token_start;   // [n_seqs + 1]
+  const int32_t *dst_first;     // [n_seqs] new position of a sequence's first, or nullptr
+  const float *rope;            // [rope_len][rope_dim] or nullptr
+  int32_t rope_len, rope_dim, interleaved;
+  int32_t layers, n_seqs, n_tokens, max_tokens, max_kv;
+  int32_t blocks_most;          // blocks of max_tokens
+  int32_t latent, turn;
+};
+
+constexpr int kCopyPlanes = 4;
+struct CopyArgs {
+  uint8_t *base;
+  int64_t piece;
+  int32_t num_pages, layers, n;
+  int32_t runs_piece;           // runs of a piece, one wave each
+  const int32_t *src, *dst;
+  uint8_t *plane[kCopyPlanes];  // [layers][num_pages][plane_bytes], or nullptr
+  int64_t plane_bytes[kCopyPlanes];
+};
+
 // Parts of at most `each` steps that `steps` steps come in.  No sum of the two,
 // which could pass 32 bits.
 constexpr int32_t parts_of_steps(int32_t steps, int32_t each) {
@@ -157,6 +197,11 @@ hipError_t launch_bounds(const KvLayer &kv, int act, int fp8, int32_t layers, in
 hipError_t launch_attend_split(const AttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_attend_chunk(const AttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs &a, int act, hipStream_t s);
+hipError_t launch_append_latent(const LatentAppendArgs &a, int act, int fp8, hipStream_t s);
+hipError_t launch_move_latents(const MoveArgs &a, int act, int fp8, hipStream_t s);
+hipError_t launch_move_tokens(const MoveArgs &a, int act, int fp8, hipStream_t s);
+int32_t copy_runs(int64_t piece);  // runs of a piece of this many bytes
+hipError_t launch_copy_pages(const CopyArgs &a, hipStream_t s);
 hipError_t launch_attend_latent(const LatentAttendArgs &a, int act, int fp8, hipStream_t s);
 hipError_t launch_select(const SelectArgs &a, int act, hipStream_t s);
 

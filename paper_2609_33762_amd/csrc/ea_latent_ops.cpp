@@ -16,20 +16,6 @@ using namespace ea::host;
 
 namespace {
 
-int check_latents(const ea_cache *c, int32_t latent, int32_t turn, int32_t dtype) {
-  if (!c || (dtype != EA_BF16 && dtype != EA_F16)) return EA_EINVAL;
-  const ea_cache_desc &d = ea::cache_desc(c);
-  if (latent < 1 || turn < 1 || d.num_kv_heads != 1 || (int64_t)latent + turn != 2LL * d.head_dim)
-    return EA_EINVAL;
-  if (d.elem_bytes != 1 && d.elem_bytes != 2) return EA_ENOTSUP;
-  if (latent % 16 != 0 || latent > ea::kMaxLatent || turn % 16 != 0 || turn > ea::kMaxTurn)
-    return EA_ENOTSUP;
-  if ((int64_t)d.num_pages * d.page_tokens > INT32_MAX) return EA_ENOTSUP;
-  // places inside a page are 32 bits
-  if (2LL * d.page_tokens * d.head_dim * d.elem_bytes > (1 << 30)) return EA_ENOTSUP;
-  return EA_OK;
-}
-
 // How an attention call is split along its tokens, and its workspace: the
 // counters, always first, then the parts.
 constexpr int64_t kCounters = ea::kArrivals * 4;
@@ -73,6 +59,44 @@ int check_attention(const ea_cache *c, const ea_batch *b, const ea_latent_attent
 }  // namespace
 
 extern "C" {
+
+int ea_append_latent(ea_cache *c, int32_t layer, const ea_batch *b, const ea_latent_append *a,
+                     hipStream_t stream) {
+  if (!a) return EA_EINVAL;
+  KV_TRY(check_latents(c, a->latent_dim, a->rope_dim, a->dtype));
+  const ea_cache_desc &d = ea::cache_desc(c);
+  KV_TRY(check_batch(d, b));
+  ea::LatentAppendArgs k{};
+  KV_TRY(layer_of(c, nullptr, layer, &k.kv));
+  if (empty(b)) return EA_OK;
+  KV_TRY(check_rows(a->latent));
+  KV_TRY(check_rows(a->key));
+  if (a->q.data) {
+    KV_TRY(check_rows(a->q));
+    KV_TRY(check_rows(a->q_out));
+    if (a->q_heads < 1) return EA_EINVAL;
+    k.q = rows(a->q);
+    k.q_out = rows(a->q_out);
+    k.q_heads = a->q_heads;
+  }
+  if (a->rope && (!aligned(a->rope, 16) || a->rope_len < b->max_kv)) return EA_EINVAL;
+  k.b = batch_rows(b);
+  k.latents = rows(a->latent);
+  k.key = rows(a->key);
+  k.rope = a->rope;
+  k.latent = a->latent_dim;
+  k.turn = a->rope_dim;
+  k.interleaved = a->interleaved;
+  k.pages_most = (int32_t)((b->max_rows + (int64_t)d.page_tokens - 2) / d.page_tokens + 1);
+  // workgroups, and waves of queries, are counted in 32 bits
+  const int64_t blocks = (int64_t)b->n_seqs * k.pages_most;
+  const int64_t queries = (int64_t)b->n_rows * ((int64_t)k.q_heads * k.turn / 2048 + 1);
+  if (blocks > INT32_MAX / 2 || queries > INT32_MAX / 2) return EA_ENOTSUP;
+  OnDevice on(ea::cache_device(c));
+  KV_HIP(on.status());
+  KV_HIP(ea::launch_append_latent(k, a->dtype, d.elem_bytes == 1, stream));
+  return EA_OK;
+}
 
 int64_t ea_attend_latent_workspace(const ea_cache *c, const ea_batch *b,
                                    const ea_latent_attention *a) {
