@@ -29,22 +29,6 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// Cosines and sines of a lane's pairs at a position.
-struct Angles {
-  f32x4 c[2], s[2];
-};
-__device__ inline Angles angles_of(const float *rope, int pos, int dim, const Place &p) {
-  Angles a = {};
-  if (p.paired) {
-    const float *cs = rope + (int64_t)pos * dim + p.d[0], *sn = cs + (dim >> 1);
-    a.c[0] = *reinterpret_cast<const f32x4 *>(cs);
-    a.c[1] = *reinterpret_cast<const f32x4 *>(cs + 4);
-    a.s[0] = *reinterpret_cast<const f32x4 *>(sn);
-    a.s[1] = *reinterpret_cast<const f32x4 *>(sn + 4);
-  }
-  return a;
-}
-
 // A lane's elements of a head, rotated for position `pos` where `rope` is not
 // null.  HALVES: the rotation, if any, pairs whole pieces; the other ways of
 // pairing need registers that this one leaves to more waves.

@@ -43,12 +43,20 @@ __device__ inline Place place_of(int lp, int D, bool turn, int dim, bool interle
   return p;
 }
 
-// Largest value over the lanes with the same place in groups of LP.
-template <int LP>
-__device__ inline float max_tokens(float v) {
-  if constexpr (LP <= 4) v = fmaxf(v, row_ror<0x124>(v));
-  if constexpr (LP <= 8) v = fmaxf(v, row_ror<0x128>(v));
-  return max_rows16(v);
+// Cosines and sines of a lane's pairs at a position.
+struct Angles {
+  f32x4 c[2], s[2];
+};
+__device__ inline Angles angles_of(const float *rope, int pos, int dim, const Place &p) {
+  Angles a = {};
+  if (p.paired) {
+    const float *cs = rope + (int64_t)pos * dim + p.d[0], *sn = cs + (dim >> 1);
+    a.c[0] = *reinterpret_cast<const f32x4 *>(cs);
+    a.c[1] = *reinterpret_cast<const f32x4 *>(cs + 4);
+    a.s[0] = *reinterpret_cast<const f32x4 *>(sn);
+    a.s[1] = *reinterpret_cast<const f32x4 *>(sn + 4);
+  }
+  return a;
 }
 
 // Four fp8 codes from four values and back.
@@ -79,37 +87,69 @@ __device__ inline void stored8(const uint8_t *p, float scale, float x[8]) {
   }
 }
 
+// Of two values, the larger over the lane and the one 32 (16) away: the first's
+// in the lower of the two, the second's in the upper.
+__device__ inline float max_halves32(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_halves16(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// Largest values of 16 elements over the lanes with the same place in groups of
+// LP: those of elements 4 * (lane / 16 in the order 0, 1, 2, 3) + 0 .. 3.
+template <int LP>
+__device__ inline void max_tokens16(const float v[16], float out[4]) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = max_halves32(v[i], v[8 + i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y = max_halves16(x[i], x[4 + i]);
+    if constexpr (LP <= 8) y = fmaxf(y, row_ror<0x128>(y));
+    if constexpr (LP <= 4) y = fmaxf(y, row_ror<0x124>(y));
+    out[i] = y;
+  }
+}
+
 // Bounds of a block's keys as whole numbers: lowest rounded down, highest
 // rounded up, in units of a power of two that holds them within 127.  LP lanes
-// hold a token's head; every (64 / LP)-th token is a lane's.  Values that are
-// not finite do not set the unit; an infinity is the largest whole number.
+// hold a token's head; every (64 / LP)-th token is a lane's, its lowest and
+// highest elements in lo and hi.  Values that are not finite do not set the
+// unit; an infinity is the largest whole number.  The reduction over tokens
+// leaves a lane four elements, whose bounds it makes and writes.
 template <int LP>
 __device__ inline void write_bounds(const KvLayer &kv, int page, int h, int lane, const Place &p,
                                     float lo[16], float hi[16]) {
   const int D = kv.head_dim;
-  float amax = 0.f;
+  const int q = lane >> 4, d = (q >> 1 ? p.d[1] : p.d[0]) + (q & 1) * 4;
+  const bool in = q >> 1 ? p.in[1] : p.in[0];
+  float l[4], u[4], amax = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    lo[i] = -max_tokens<LP>(-lo[i]);
-    hi[i] = max_tokens<LP>(hi[i]);
-    if (p.in[i >> 3] && finite(lo[i])) amax = fmaxf(amax, fabsf(lo[i]));
-    if (p.in[i >> 3] && finite(hi[i])) amax = fmaxf(amax, fabsf(hi[i]));
+  for (int i = 0; i < 16; ++i) lo[i] = -lo[i];
+  max_tokens16<LP>(lo, l);
+  max_tokens16<LP>(hi, u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (in && finite(l[i])) amax = fmaxf(amax, fabsf(l[i]));
+    if (in && finite(u[i])) amax = fmaxf(amax, fabsf(u[i]));
   }
   const float s = int8_scale(max_wave(amax)), inv = power_inverse(s);
+  if (in && (lane & 15) < LP) {
+    uint32_t wl = 0, wh = 0;
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    if (lane >= LP || !p.in[n]) continue;
-    u32x2 wl = {0, 0}, wh = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int l = (int)fmaxf(fminf(floorf(lo[n * 8 + i] * inv), 127.f), -127.f);
-      const int u = (int)fmaxf(fminf(ceilf(hi[n * 8 + i] * inv), 127.f), -127.f);
-      wl[i >> 2] |= (uint32_t)(uint8_t)l << (8 * (i & 3));
-      wh[i >> 2] |= (uint32_t)(uint8_t)u << (8 * (i & 3));
+    for (int i = 0; i < 4; ++i) {
+      const int a = (int)fmaxf(fminf(floorf(-l[i] * inv), 127.f), -127.f);
+      const int b = (int)fmaxf(fminf(ceilf(u[i] * inv), 127.f), -127.f);
+      wl |= (uint32_t)(uint8_t)a << (8 * i);
+      wh |= (uint32_t)(uint8_t)b << (8 * i);
     }
-    int8_t *q = kv.bounds + ((int64_t)page * 2 * kv.heads + h) * D + p.d[n];
-    *reinterpret_cast<u32x2 *>(q) = wl;
-    *reinterpret_cast<u32x2 *>(q + (int64_t)kv.heads * D) = wh;
+    int8_t *to = kv.bounds + ((int64_t)page * 2 * kv.heads + h) * D + d;
+    *reinterpret_cast<uint32_t *>(to) = wl;
+    *reinterpret_cast<uint32_t *>(to + (int64_t)kv.heads * D) = wh;
   }
   if (lane == 0) kv.bound_scales[(int64_t)page * kv.heads + h] = s;
 }

@@ -138,6 +138,7 @@ struct MoveArgs {
   int32_t rope_len, rope_dim, interleaved;
   int32_t layers, n_seqs, n_tokens, max_tokens, max_kv;
   int32_t blocks_most;          // blocks of max_tokens
+  int32_t layers_wave;          // layers that one wave (workgroup) goes through
   int32_t latent, turn;
 };
 

@@ -62,43 +62,14 @@ __global__ __launch_bounds__(kThreads) void copy_pages(CopyArgs a, int64_t runs,
   }
 }
 
-// A lane's elements of a stored head in 32 bits, turned by |position| `at`
-// where rope is not null.
+// Elements of a stored head beside the ones that a lane holds, for the ways of
+// pairing whose halves are no whole pieces: x turned by |position| `at`.
 template <int ACT, bool FP8>
-__device__ inline void turned(const uint8_t *head, const Place &p, const float *rope, int at,
-                              float sign, int dim, bool interleaved, float scale, float x[16]) {
+__device__ inline void turn_apart(const uint8_t *head, const Place &p, const float *rope, int at,
+                                  float sign, int dim, bool interleaved, float x[16]) {
 #pragma clang fp contract(off)
-  constexpr int EB = FP8 ? 1 : 2;
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    if (p.in[n]) {
-      stored8<ACT, FP8>(head + p.d[n] * EB, scale, x + n * 8);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[n * 8 + i] = 0.f;
-    }
-  }
-  if (!rope) return;
   const int half = dim >> 1;
   const float *cs = rope + (int64_t)at * dim, *sn = cs + half;
-  if (p.paired) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float co = cs[p.d[0] + i], si = sn[p.d[0] + i] * sign, a = x[i], b = x[8 + i];
-      const float ac = a * co, bs = b * si, bc = b * co, as = a * si;
-      x[i] = ac - bs;
-      x[8 + i] = bc + as;
-    }
-    return;
-  }
-  auto one = [&](int d) {  // element d as it is stored
-    if constexpr (FP8) {
-      const f32x2 v = __builtin_amdgcn_cvt_pk_f32_fp8(head[d], false);
-      return v[0] * scale;
-    } else {
-      return act_to_float<ACT>(reinterpret_cast<const uint16_t *>(head)[d]);
-    }
-  };
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     if (!p.in[n] || p.d[n] >= dim) continue;
@@ -108,144 +79,296 @@ __device__ inline void turned(const uint8_t *head, const Place &p, const float *
       if (d >= dim) break;
       const bool upper = interleaved ? d & 1 : d >= half;
       const int f = interleaved ? d >> 1 : upper ? d - half : d;
-      const float y = one(interleaved ? d ^ 1 : upper ? d - half : d + half);
+      const int e = interleaved ? d ^ 1 : upper ? d - half : d + half;
+      float y;
+      if constexpr (FP8) y = __builtin_amdgcn_cvt_pk_f32_fp8(head[e], false)[0];
+      else y = act_to_float<ACT>(reinterpret_cast<const uint16_t *>(head)[e]);
       const float xc = x[n * 8 + i] * cs[f], ys = y * (sn[f] * sign);
       x[n * 8 + i] = upper ? xc + ys : xc - ys;
     }
   }
 }
 
-// One wave: one block of one layer, for one KV head, keys or values.
-template <int ACT, bool FP8, int LP>
-__global__ __launch_bounds__(kThreads) void move_tokens(MoveArgs a, int64_t units) {
+// One wave: one block in some layers, all KV heads, keys and values.  Where its
+// tokens are, and the angles that they turn by, serve all of them; the next
+// head's elements load while this one's are turned and written.  HALVES: the
+// turn, if any, pairs whole pieces of 8.  ONE: a block is 16 tokens at most,
+// which registers hold; otherwise the ones after them are read again for each
+// use.
+template <int ACT, bool FP8, int LP, bool HALVES, bool ONE>
+__global__ __launch_bounds__(kThreads) void move_tokens(MoveArgs a, uint32_t units) {
   constexpr int EB = FP8 ? 1 : 2, TW = kLanes / LP;  // tokens of a pass
-  constexpr int KEEP = 2;  // passes whose tokens stay in registers
+  constexpr int KEEP = 16 / TW;  // passes whose tokens stay in registers
+  constexpr int W = FP8 ? 2 : 4;  // words of 8 elements
   const int lane = threadIdx.x & 63;
-  int64_t u = (int64_t)blockIdx.x * kWaves + uniform((int)threadIdx.x >> 6);
+  uint32_t u = blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
   if (u >= units) return;
-  KvLayer kv = a.kv;
-  const int H = kv.heads, D = kv.head_dim;
-  const int h = u % H;
-  u /= H;
-  const bool value = u & 1;
-  u >>= 1;
   const int j = u % a.blocks_most;
   u /= a.blocks_most;
-  const int s = u % a.n_seqs;
-  const int64_t layer = u / a.n_seqs;
+  const int s = u % a.n_seqs, layer0 = u / a.n_seqs * a.layers_wave;
+  const int layer1 = min(layer0 + a.layers_wave, a.layers);
   const MovedBlock m = moved_block(a, s, j);
   if (m.n <= 0) return;
-  kv.base += layer * a.layer_bytes;
-  if (FP8) kv.scales += layer * a.layer_scales;
-  if (kv.bounds) {
-    kv.bounds += layer * kv.num_pages * 2 * H * D;
-    kv.bound_scales += layer * kv.num_pages * H;
-  }
-  const int64_t token_bytes = (int64_t)H * D * EB;
+  const int H = a.kv.heads, D = a.kv.head_dim;
+  const uint32_t token_bytes = H * D * EB, half_piece = (uint32_t)(a.kv.piece >> 1);
   const int t0 = lane / LP;
-  const float *rope = value ? nullptr : a.rope;
-  const Place at = place_of(lane % LP, D, rope != nullptr, a.rope_dim, a.interleaved);
-  const int64_t head_at = (value ? kv.piece >> 1 : 0) + (int64_t)h * D * EB;
-  uint8_t *dst = kv.base + m.page * kv.piece + head_at;
-  auto fetch = [&](int i, float x[16]) {
-    const MovedToken t = moved_token(a, m, i);
-    if (t.page < 0) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) x[k] = 0.f;
-      return;
+  const bool with_bounds = a.kv.bounds != nullptr;
+  const Place at = place_of(lane % LP, D, a.rope != nullptr, a.rope_dim, a.interleaved);
+
+  MovedToken tok[KEEP];
+  Angles an[KEEP];
+  auto angles = [&](const MovedToken &t) {
+    Angles g = {};
+    if (HALVES && t.by != 0) g = angles_of(a.rope, abs(t.by), a.rope_dim, at);
+    if (t.by < 0) {
+      g.s[0] = -g.s[0];
+      g.s[1] = -g.s[1];
     }
-    float scale = 1.f;
-    if (FP8)
-      scale = kv.scales[(int64_t)t.page * kv.scale_page + (value ? kv.scale_kv : 0) +
-                        h * kv.scale_head];
-    turned<ACT, FP8>(kv.base + t.page * kv.piece + head_at + t.slot * token_bytes, at,
-                     t.by ? rope : nullptr, abs(t.by), t.by < 0 ? -1.f : 1.f, a.rope_dim,
-                     a.interleaved, scale, x);
+    return g;
   };
-  float x[KEEP][16];
 #pragma unroll
-  for (int k = 0; k < KEEP; ++k)
-    if (t0 + k * TW < m.n) fetch(t0 + k * TW, x[k]);
-  float scale = 1.f, inv = 1.f;
-  if constexpr (FP8) {
-    float amax = 0.f;
-    auto largest = [&](const float y[16]) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (finite(y[i])) amax = fmaxf(amax, fabsf(y[i]));
-    };
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k)
-      if (t0 + k * TW < m.n) largest(x[k]);
-    for (int t = t0 + KEEP * TW; t < m.n; t += TW) {
-      float y[16];
-      fetch(t, y);
-      largest(y);
+  for (int k = 0; k < KEEP; ++k) {
+    tok[k] = {-1, 0, 0};
+    if (t0 + k * TW < m.n) tok[k] = moved_token(a, m, t0 + k * TW);
+    an[k] = angles(tok[k]);
+  }
+
+  for (int layer = layer0; layer < layer1; ++layer) {
+    KvLayer kv = a.kv;
+    kv.base += layer * a.layer_bytes;
+    if (FP8) kv.scales += layer * a.layer_scales;
+    if (with_bounds) {
+      kv.bounds += (int64_t)layer * kv.num_pages * 2 * H * D;
+      kv.bound_scales += (int64_t)layer * kv.num_pages * H;
     }
-    scale = fp8_scale(max_wave(amax));
-    inv = power_inverse(scale);
-    if (lane == 0)
-      kv.scales[(int64_t)m.page * kv.scale_page + (value ? kv.scale_kv : 0) + h * kv.scale_head] =
-          scale;
-  }
-  const bool bounds = !value && kv.bounds;
-  float lo[16], hi[16];
+    // planes: keys of head plane / 2, then its values
+    auto head_at = [&](int plane) { return (plane & 1 ? half_piece : 0) + (plane >> 1) * D * EB; };
+    struct Raw {
+      uint32_t w[2][W];
+      float scale;
+    };
+    auto load = [&](const MovedToken &t, int plane) {
+      Raw r = {};
+      r.scale = 1.f;
+      if (t.page < 0) return r;
+      const uint8_t *p = kv.base + ((uint64_t)t.page * kv.piece + t.slot * token_bytes +
+                                    head_at(plane));
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    lo[i] = __builtin_inff();
-    hi[i] = kNegInf;
-  }
-  auto store = [&](int t, const float y[16]) {
+      for (int n = 0; n < 2; ++n) {
+        if (!at.in[n]) continue;
+        if constexpr (FP8) {
+          const u32x2 v = *reinterpret_cast<const u32x2 *>(p + at.d[n]);
+          r.w[n][0] = v[0];
+          r.w[n][1] = v[1];
+        } else {
+          const u32x4 v = *reinterpret_cast<const u32x4 *>(p + at.d[n] * 2);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      if (!at.in[n]) continue;
-      uint8_t *q = dst + t * token_bytes + at.d[n] * EB;
-      float z[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = FP8 ? y[n * 8 + i] * inv : y[n * 8 + i];
-      if constexpr (FP8) {
-        const u32x2 w = {fp8_word(z[0], z[1], z[2], z[3]), fp8_word(z[4], z[5], z[6], z[7])};
-        *reinterpret_cast<u32x2 *>(q) = w;
-        fp8_values(w[0], z);
-        fp8_values(w[1], z + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] *= scale;
-      } else {
-        const u32x4 w = {pack_act<ACT>(z[0], z[1]), pack_act<ACT>(z[2], z[3]),
-                         pack_act<ACT>(z[4], z[5]), pack_act<ACT>(z[6], z[7])};
-        *reinterpret_cast<u32x4 *>(q) = w;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          z[i] = act_to_float<ACT>((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
-      }
-      if (bounds) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          lo[n * 8 + i] = fminf(lo[n * 8 + i], z[i]);
-          hi[n * 8 + i] = fmaxf(hi[n * 8 + i], z[i]);
+          for (int i = 0; i < 4; ++i) r.w[n][i] = v[i];
         }
       }
-    }
-  };
+      if (FP8)
+        r.scale = kv.scales[(int64_t)t.page * kv.scale_page + (plane & 1 ? kv.scale_kv : 0) +
+                            (plane >> 1) * kv.scale_head];
+      return r;
+    };
+    // Elements as stored (fp8: codes, their scale apart), turned.
+    auto values = [&](const Raw &r, const MovedToken &t, const Angles &g, int plane, float x[16]) {
+#pragma clang fp contract(off)
 #pragma unroll
-  for (int k = 0; k < KEEP; ++k)
-    if (t0 + k * TW < m.n) store(t0 + k * TW, x[k]);
-  for (int t = t0 + KEEP * TW; t < m.n; t += TW) {
-    float y[16];
-    fetch(t, y);
-    store(t, y);
+      for (int n = 0; n < 2; ++n) {
+        if constexpr (FP8) {
+          fp8_values(r.w[n][0], x + n * 8);
+          fp8_values(r.w[n][1], x + n * 8 + 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            x[n * 8 + i] = act_to_float<ACT>((uint16_t)(r.w[n][i >> 1] >> (16 * (i & 1))));
+        }
+      }
+      if ((plane & 1) || t.by == 0) return;
+      if constexpr (HALVES) {
+        if (at.paired) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float co = g.c[i >> 2][i & 3], si = g.s[i >> 2][i & 3], y = x[i], z = x[8 + i];
+            const float yc = y * co, zs = z * si, zc = z * co, ys = y * si;
+            x[i] = yc - zs;
+            x[8 + i] = zc + ys;
+          }
+        }
+      } else {
+        turn_apart<ACT, FP8>(kv.base + ((uint64_t)t.page * kv.piece + t.slot * token_bytes +
+                                        head_at(plane)),
+                             at, a.rope, abs(t.by), t.by < 0 ? -1.f : 1.f, a.rope_dim,
+                             a.interleaved, x);
+      }
+    };
+    // of a token that no register holds
+    auto fetch = [&](int i, int plane, float x[16]) {
+      const MovedToken t = moved_token(a, m, i);
+      const Raw r = load(t, plane);
+      values(r, t, angles(t), plane, x);
+      return r.scale;
+    };
+
+    Raw next[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) next[k] = load(tok[k], 0);
+    for (int plane = 0; plane < 2 * H; ++plane) {
+      const bool value = plane & 1, bounds = !value && with_bounds;
+      const int h = plane >> 1;
+      uint8_t *dst = kv.base + ((uint64_t)m.page * kv.piece + head_at(plane));
+      if constexpr (!FP8) {  // nothing of values changes
+        if (value) {
+          Raw now[KEEP];
+#pragma unroll
+          for (int k = 0; k < KEEP; ++k) {
+            now[k] = next[k];
+            if (plane + 1 < 2 * H) next[k] = load(tok[k], plane + 1);
+          }
+          auto put = [&](int t, const Raw &r) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              if (at.in[n])
+                *reinterpret_cast<u32x4 *>(dst + t * token_bytes + at.d[n] * 2) =
+                    u32x4{r.w[n][0], r.w[n][1], r.w[n][2], r.w[n][3]};
+          };
+#pragma unroll
+          for (int k = 0; k < KEEP; ++k)
+            if (t0 + k * TW < m.n) put(t0 + k * TW, now[k]);
+          if constexpr (!ONE)
+            for (int t = t0 + KEEP * TW; t < m.n; t += TW) put(t, load(moved_token(a, m, t), plane));
+          continue;
+        }
+      }
+      float x[KEEP][16], scales[KEEP];
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k) {
+        values(next[k], tok[k], an[k], plane, x[k]);
+        scales[k] = next[k].scale;
+        if (plane + 1 < 2 * H) next[k] = load(tok[k], plane + 1);
+      }
+      float scale = 1.f, inv = 1.f;
+      if constexpr (FP8) {
+        // of all values first: max passes over NaN, and infinities are rare
+        auto largest = [&](const float y[16], float by) {
+          float v = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) v = fmaxf(fmaxf(v, fabsf(y[i])), fabsf(y[i + 1]));
+          return v * fabsf(by);
+        };
+        auto largest_finite = [&](const float y[16], float by) {
+          float v = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v = fmaxf(v, finite(y[i] * by) ? fabsf(y[i] * by) : 0.f);
+          return v;
+        };
+        auto over = [&](auto of) {
+          float v = 0.f;
+#pragma unroll
+          for (int k = 0; k < KEEP; ++k) v = fmaxf(v, of(x[k], scales[k]));  // zeros past the last
+          if constexpr (!ONE)
+            for (int t = t0 + KEEP * TW; t < m.n; t += TW) {
+              float y[16];
+              const float by = fetch(t, plane, y);
+              v = fmaxf(v, of(y, by));
+            }
+          return max_wave(v);
+        };
+        float amax = over(largest);
+        if (!finite(amax)) amax = over(largest_finite);
+        scale = fp8_scale(amax);
+        inv = power_inverse(scale);
+        if (lane == 0)
+          kv.scales[(int64_t)m.page * kv.scale_page + (value ? kv.scale_kv : 0) +
+                    h * kv.scale_head] = scale;
+      }
+      float lo[16], hi[16];
+      if (bounds) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          lo[i] = __builtin_inff();
+          hi[i] = kNegInf;
+        }
+      }
+      auto store = [&](int t, float y[16], float by) {
+        const float f = by * inv;  // exact: inv is a power of two
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          if (!at.in[n]) continue;
+          uint8_t *q = dst + t * token_bytes + at.d[n] * EB;
+          float z[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = FP8 ? y[n * 8 + i] * f : y[n * 8 + i];
+          if constexpr (FP8) {
+            const u32x2 w = {fp8_word(z[0], z[1], z[2], z[3]), fp8_word(z[4], z[5], z[6], z[7])};
+            *reinterpret_cast<u32x2 *>(q) = w;
+            if (bounds) {
+              fp8_values(w[0], z);
+              fp8_values(w[1], z + 4);
+            }
+          } else {
+            const u32x4 w = {pack_act<ACT>(z[0], z[1]), pack_act<ACT>(z[2], z[3]),
+                             pack_act<ACT>(z[4], z[5]), pack_act<ACT>(z[6], z[7])};
+            *reinterpret_cast<u32x4 *>(q) = w;
+            if (bounds) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                z[i] = act_to_float<ACT>((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
+            }
+          }
+          if (bounds) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              lo[n * 8 + i] = fminf(lo[n * 8 + i], z[i]);
+              hi[n * 8 + i] = fmaxf(hi[n * 8 + i], z[i]);
+            }
+          }
+        }
+      };
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (t0 + k * TW < m.n) store(t0 + k * TW, x[k], scales[k]);
+      if constexpr (!ONE)
+        for (int t = t0 + KEEP * TW; t < m.n; t += TW) {
+          float y[16];
+          const float by = fetch(t, plane, y);
+          store(t, y, by);
+        }
+      if (bounds) {
+        if constexpr (FP8) {  // of codes until here, all in units of the scale
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            lo[i] *= scale;
+            hi[i] *= scale;
+          }
+        }
+        write_bounds<LP>(kv, m.page, h, lane, at, lo, hi);
+      }
+    }
   }
-  if (bounds) write_bounds<LP>(kv, m.page, h, lane, at, lo, hi);
+}
+
+template <int ACT, bool FP8, int LP>
+void move_as(const MoveArgs &a, hipStream_t s) {
+  const uint32_t units = (uint32_t)((a.layers + a.layers_wave - 1) / a.layers_wave * a.n_seqs *
+                                    a.blocks_most);
+  const dim3 grid((units + kWaves - 1) / kWaves), block(kThreads);
+  const bool halves = !a.rope || (!a.interleaved && a.rope_dim % 16 == 0);
+  if (!halves)
+    hipLaunchKernelGGL((move_tokens<ACT, FP8, LP, false, false>), grid, block, 0, s, a, units);
+  else if (a.kv.page_tokens <= 16)
+    hipLaunchKernelGGL((move_tokens<ACT, FP8, LP, true, true>), grid, block, 0, s, a, units);
+  else
+    hipLaunchKernelGGL((move_tokens<ACT, FP8, LP, true, false>), grid, block, 0, s, a, units);
 }
 
 template <int ACT, bool FP8>
 hipError_t move(const MoveArgs &a, hipStream_t s) {
-  const int64_t units = (int64_t)a.layers * a.n_seqs * a.blocks_most * 2 * a.kv.heads;
-  const dim3 grid((unsigned)((units + kWaves - 1) / kWaves)), block(kThreads);
   switch (lanes_of(a.kv.head_dim)) {
-    case 4: hipLaunchKernelGGL((move_tokens<ACT, FP8, 4>), grid, block, 0, s, a, units); break;
-    case 8: hipLaunchKernelGGL((move_tokens<ACT, FP8, 8>), grid, block, 0, s, a, units); break;
-    default: hipLaunchKernelGGL((move_tokens<ACT, FP8, 16>), grid, block, 0, s, a, units);
+    case 4: move_as<ACT, FP8, 4>(a, s); break;
+    case 8: move_as<ACT, FP8, 8>(a, s); break;
+    default: move_as<ACT, FP8, 16>(a, s);
   }
   return hipGetLastError();
 }

@@ -2,6 +2,7 @@
 // and the launches.  They allocate nothing.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstdint>
 
@@ -101,11 +102,13 @@ int ea_move_tokens(ea_cache *c, const ea_cache_planes *planes, int32_t layer_beg
   k.max_tokens = a->max_tokens;
   k.max_kv = a->max_kv;
   k.blocks_most = (int32_t)((a->max_tokens + T - 1) / T);
+  const int64_t blocks = (int64_t)a->n_seqs * k.blocks_most;
+  k.layers_wave = (int32_t)std::min<int64_t>(
+      layer_count, std::max<int64_t>(1, blocks * layer_count / 8192));
   k.latent = a->latent_dim;
   k.turn = a->rope_dim;
   // workgroups and waves are counted in 32 bits
-  if ((int64_t)a->n_seqs * k.blocks_most > INT32_MAX / 8 / d.num_kv_heads / layer_count)
-    return EA_ENOTSUP;
+  if (blocks > INT32_MAX / layer_count) return EA_ENOTSUP;
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());
   const int fp8 = d.elem_bytes == 1;
