@@ -154,26 +154,27 @@ __device__ inline void write_bounds(const KvLayer &kv, int page, int h, int lane
   if (lane == 0) kv.bound_scales[(int64_t)page * kv.heads + h] = s;
 }
 
-// Block j of a sequence's moved tokens: its page, n tokens from list place `at`
-// on, their first new position.  n 0: nothing to write.
+// A sequence's moved tokens from `first` on, `most` at most: n tokens from list
+// place `at` on, their first new position; n 0: none.  Of a block, its page too.
 struct MovedBlock {
   int32_t page, n, at;
   int64_t pos;
   const int32_t *table;  // of the old pages
 };
-__device__ inline MovedBlock moved_block(const MoveArgs &a, int s, int j) {
-  MovedBlock m = {-1, 0, 0, 0, a.src_table + (int64_t)s * a.src_stride};
-  const int T = a.kv.page_tokens;
+__device__ inline MovedBlock moved_run(const MoveArgs &a, int s, int first, int most) {
   const int lo = min(max(a.token_start[s], 0), a.n_tokens);
   const int hi = min(max(a.token_start[s + 1], lo), a.n_tokens);
-  const int first = j * T, n = min(min(hi - lo, a.max_tokens) - first, T);
-  if (n <= 0) return m;
+  MovedBlock m = {-1, min(min(hi - lo, a.max_tokens) - first, most), lo + first,
+                  (int64_t)(a.dst_first ? a.dst_first[s] : 0) + first,
+                  a.src_table + (int64_t)s * a.src_stride};
+  return m;
+}
+__device__ inline MovedBlock moved_block(const MoveArgs &a, int s, int j) {
+  MovedBlock m = moved_run(a, s, j * a.kv.page_tokens, a.kv.page_tokens);
+  if (m.n <= 0) return m;
   const int page = a.dst_table[(int64_t)s * a.dst_stride + j];
-  if ((uint32_t)page >= (uint32_t)a.kv.num_pages) return m;
+  if ((uint32_t)page >= (uint32_t)a.kv.num_pages) m.n = 0;
   m.page = page;
-  m.n = n;
-  m.at = lo + first;
-  m.pos = (int64_t)(a.dst_first ? a.dst_first[s] : 0) + first;
   return m;
 }
 

@@ -237,37 +237,238 @@ __global__ __launch_bounds__(kThreads) void append_latent(LatentAppendArgs a, ui
   }
 }
 
+// Moved rows: a workgroup takes up to 16 tokens (fp8: a block, 16 tokens at a
+// time) through some layers.  A thread has 16-byte pieces of their latents, which
+// only fp8 looks into, and one piece of 8 turned elements, with the piece that
+// it turns with and its angles, which serve all layers.
 template <int ACT, bool FP8>
 __global__ __launch_bounds__(kThreads) void move_latents(MoveArgs a) {
-  constexpr int EB = FP8 ? 1 : 2;
-  KvLayer kv = a.kv;
-  const int T = kv.page_tokens, C = a.latent, R = a.turn;
+  constexpr int EB = FP8 ? 1 : 2, PER = 16 / EB;  // elements of a piece
+  constexpr int KEEP = 16 * kMaxLatent / PER / kThreads;
+  constexpr int W = FP8 ? 2 : 4;                  // words of 8 elements
+  __shared__ float most[2][kWaves][2];
+  const int T = a.kv.page_tokens, C = a.latent, R = a.turn, tid = threadIdx.x;
+  const uint32_t row_bytes = (C + R) * EB;
   uint32_t u = blockIdx.x;
   const int j = u % a.blocks_most;
   u /= a.blocks_most;
-  const int s = u % a.n_seqs, layer = u / a.n_seqs;
-  kv.base += layer * a.layer_bytes;
-  if (FP8) kv.scales += layer * a.layer_scales;
-  const MovedBlock m = moved_block(a, s, j);
+  const int s = u % a.n_seqs, layer0 = u / a.n_seqs * a.layers_wave;
+  const int layer1 = min(layer0 + a.layers_wave, a.layers);
+  // fp8: the block's tokens; else 16 of the sequence, whose blocks they are in
+  // is looked up for each
+  MovedBlock m;
+  if constexpr (FP8) m = moved_block(a, s, j);
+  else m = moved_run(a, s, j * 16, 16);
   if (m.n <= 0) return;
-  const int64_t row_bytes = (int64_t)(C + R) * EB;
-  auto fetch = [&](int i, int piece, float x[8]) {
-    const MovedToken t = moved_token(a, m, i);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = 0.f;
-    if (t.page < 0) return;
-    const uint8_t *row = kv.base + t.page * kv.piece + t.slot * row_bytes;
-    const int rp = piece - (C >> 3);
-    const float scale = FP8 ? kv.scales[(int64_t)t.page * 2 + (rp < 0 ? 0 : 1)] : 1.f;
-    stored8<ACT, FP8>(row + piece * 8 * EB, scale, x);
-    if (rp >= 0 && a.rope && t.by != 0)
-      turn_piece(x, rp, a.rope, abs(t.by), t.by < 0 ? -1.f : 1.f, R, a.interleaved,
-                 [&](int of, float y[8]) {
-                   stored8<ACT, FP8>(row + (C + of * 8) * EB, scale, y);
-                 });
+  const int32_t *dst_table = a.dst_table + (int64_t)s * a.dst_stride;
+  const int groups = FP8 ? (m.n + 15) / 16 : 1;
+
+  const int lat = C / PER, trn = R >> 3, half = trn >> 1;  // pieces of a token
+  // place in the layer that a piece comes from (-1: zeros) and goes to (-1: nowhere)
+  int64_t src[KEEP], dst[KEEP], tsrc, tdst;
+  uint32_t src_page[KEEP], tsrc_page;
+  int tby = 0, apart = 0;  // the turn, and the other piece's distance in bytes
+  f32x4 c[2], sn[2];
+  bool upper = false;
+  auto to_of = [&](int i) -> int64_t {  // row that token i goes to
+    if constexpr (FP8) return m.page * a.kv.piece + (int64_t)i * row_bytes;
+    const int at = j * 16 + i, e = over_page(a.kv, at);
+    const int page = dst_table[e];
+    if ((uint32_t)page >= (uint32_t)a.kv.num_pages) return -1;
+    return page * a.kv.piece + (int64_t)(at - e * T) * row_bytes;
   };
-  write_block<ACT, FP8>(kv.base + m.page * kv.piece,
-                        FP8 ? kv.scales + (int64_t)m.page * 2 : nullptr, 0, m.n, C, R, fetch);
+  auto places = [&](int group) {
+    const int n = min(m.n - group * 16, 16);
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) {
+      const int at = tid + k * kThreads, i = at / lat, piece = at - i * lat;
+      src[k] = dst[k] = -1;
+      src_page[k] = 0;
+      if (i >= n) continue;
+      const MovedToken t = moved_token(a, m, group * 16 + i);
+      const int64_t to = to_of(group * 16 + i);
+      if (to >= 0) dst[k] = to + piece * 16;
+      if (t.page < 0) continue;
+      src_page[k] = t.page;
+      src[k] = t.page * a.kv.piece + (int64_t)t.slot * row_bytes + piece * 16;
+    }
+    tsrc = tdst = -1;
+    tsrc_page = 0;
+    const int i = tid / trn, piece = tid - i * trn;
+    if (i >= n) return;
+    const MovedToken t = moved_token(a, m, group * 16 + i);
+    const int64_t to = to_of(group * 16 + i);
+    if (to >= 0) tdst = to + C * EB + piece * 8 * EB;
+    if (t.page < 0) return;
+    tsrc_page = t.page;
+    tsrc = t.page * a.kv.piece + (int64_t)t.slot * row_bytes + C * EB + piece * 8 * EB;
+    tby = t.by;
+    if (tby == 0) return;
+    upper = piece >= half;
+    apart = a.interleaved ? 0 : (upper ? -half : half) * 8 * EB;
+    const float *cs = a.rope + (int64_t)abs(tby) * R + (a.interleaved ? piece * 4
+                                                        : (upper ? piece - half : piece) * 8);
+    const float *ss = cs + (R >> 1);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int more = a.interleaved ? 0 : q * 4;  // four pairs then
+      c[q] = *reinterpret_cast<const f32x4 *>(cs + more);
+      sn[q] = *reinterpret_cast<const f32x4 *>(ss + more);
+      if (tby < 0) sn[q] = -sn[q];
+    }
+  };
+  struct Raw {
+    u32x4 lat[KEEP];
+    float lat_scale[KEEP], turn_scale;
+    uint32_t own[W], other[W];
+  };
+  auto load8 = [&](const uint8_t *p, uint32_t w[W]) {
+    if constexpr (FP8) {
+      const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+      w[0] = v[0];
+      w[1] = v[1];
+    } else {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = v[i];
+    }
+  };
+  auto load = [&](int layer) {
+    Raw r = {};
+    const uint8_t *base = a.kv.base + layer * a.layer_bytes;
+    const float *scales = FP8 ? a.kv.scales + layer * a.layer_scales : nullptr;
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) {
+      r.lat_scale[k] = 0.f;
+      if (src[k] >= 0) {
+        r.lat[k] = *reinterpret_cast<const u32x4 *>(base + src[k]);
+        if (FP8) r.lat_scale[k] = scales[(int64_t)src_page[k] * 2];
+      }
+    }
+    r.turn_scale = 0.f;
+    if (tsrc >= 0) {
+      load8(base + tsrc, r.own);
+      if (tby != 0) load8(base + tsrc + apart, r.other);
+      if (FP8) r.turn_scale = scales[(int64_t)tsrc_page * 2 + 1];
+    }
+    return r;
+  };
+  auto values8 = [&](const uint32_t w[W], float x[8]) {
+    if constexpr (FP8) {
+      fp8_values(w[0], x);
+      fp8_values(w[1], x + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = act_to_float<ACT>((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
+    }
+  };
+  // the turned piece, fp8 without its scale
+  auto turned = [&](const Raw &r, float x[8]) {
+    values8(r.own, x);
+    if (tby == 0) return;
+    float y[8];
+    values8(r.other, y);
+    const float co[8] = {c[0][0], c[0][1], c[0][2], c[0][3], c[1][0], c[1][1], c[1][2], c[1][3]};
+    const float si[8] = {sn[0][0], sn[0][1], sn[0][2], sn[0][3],
+                         sn[1][0], sn[1][1], sn[1][2], sn[1][3]};
+    if (a.interleaved) turn8<true>(x, y, co, si, false, 1.f);
+    else turn8<false>(x, y, co, si, upper, 1.f);
+  };
+
+  if (groups == 1) places(0);
+  if constexpr (!FP8) {
+    Raw next = load(layer0);
+    for (int layer = layer0; layer < layer1; ++layer) {
+      const Raw r = next;
+      if (layer + 1 < layer1) next = load(layer + 1);
+      uint8_t *base = a.kv.base + layer * a.layer_bytes;
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (dst[k] >= 0) *reinterpret_cast<u32x4 *>(base + dst[k]) = r.lat[k];
+      if (tdst < 0) continue;
+      u32x4 w = {r.own[0], r.own[1], r.own[2], r.own[3]};
+      if (tby != 0) {
+        float x[8];
+        turned(r, x);
+        w = u32x4{pack_act<ACT>(x[0], x[1]), pack_act<ACT>(x[2], x[3]), pack_act<ACT>(x[4], x[5]),
+                  pack_act<ACT>(x[6], x[7])};
+      }
+      *reinterpret_cast<u32x4 *>(base + tdst) = w;
+    }
+  } else {
+    for (int layer = layer0; layer < layer1; ++layer) {
+      uint8_t *base = a.kv.base + layer * a.layer_bytes;
+      float amax[2] = {0.f, 0.f};
+      Raw r;
+      for (int group = 0; group < groups; ++group) {
+        if (groups > 1) places(group);
+        r = load(layer);
+        auto largest = [&](const float *x, int n, float by) {
+          float v = 0.f;
+#pragma unroll
+          for (int i = 0; i < n; ++i) {
+            const float y = fabsf(x[i] * by);
+            v = fmaxf(v, finite(y) ? y : 0.f);
+          }
+          return v;
+        };
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+          float x[16];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) fp8_values(r.lat[k][i], x + 4 * i);
+          amax[0] = fmaxf(amax[0], largest(x, 16, r.lat_scale[k]));
+        }
+        float x[8];
+        turned(r, x);
+        amax[1] = fmaxf(amax[1], largest(x, 8, r.turn_scale));
+      }
+      float (*to)[2] = most[layer & 1];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        amax[w] = max_wave(amax[w]);
+        if ((tid & 63) == 0) to[tid >> 6][w] = amax[w];
+      }
+      __syncthreads();
+      float inv[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        float v = to[0][w];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) v = fmaxf(v, to[i][w]);
+        const float scale = fp8_scale(v);
+        inv[w] = power_inverse(scale);
+        if (tid == 0) a.kv.scales[layer * a.layer_scales + (int64_t)m.page * 2 + w] = scale;
+      }
+      for (int group = 0; group < groups; ++group) {
+        if (groups > 1) {
+          places(group);
+          r = load(layer);
+        }
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+          if (dst[k] < 0) continue;
+          const float f = r.lat_scale[k] * inv[0];
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x[4];
+            fp8_values(r.lat[k][i], x);
+            w[i] = fp8_word(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+          }
+          *reinterpret_cast<u32x4 *>(base + dst[k]) = w;
+        }
+        if (tdst >= 0) {
+          const float f = r.turn_scale * inv[1];
+          float x[8];
+          turned(r, x);
+          *reinterpret_cast<u32x2 *>(base + tdst) =
+              u32x2{fp8_word(x[0] * f, x[1] * f, x[2] * f, x[3] * f),
+                    fp8_word(x[4] * f, x[5] * f, x[6] * f, x[7] * f)};
+        }
+      }
+    }
+  }
 }
 
 template <int ACT, bool FP8>
@@ -285,7 +486,8 @@ hipError_t append(const LatentAppendArgs &a, hipStream_t s) {
 
 template <int ACT, bool FP8>
 hipError_t move(const MoveArgs &a, hipStream_t s) {
-  const int64_t grid = (int64_t)a.layers * a.n_seqs * a.blocks_most;
+  const int64_t grid =
+      (int64_t)(a.layers + a.layers_wave - 1) / a.layers_wave * a.n_seqs * a.blocks_most;
   hipLaunchKernelGGL((move_latents<ACT, FP8>), dim3((unsigned)grid), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }

@@ -101,7 +101,9 @@ int ea_move_tokens(ea_cache *c, const ea_cache_planes *planes, int32_t layer_beg
   k.n_tokens = a->n_tokens;
   k.max_tokens = a->max_tokens;
   k.max_kv = a->max_kv;
-  k.blocks_most = (int32_t)((a->max_tokens + T - 1) / T);
+  // 16-bit latents go 16 tokens at a time, whatever block they are in
+  const int64_t unit = latents && d.elem_bytes == 2 ? 16 : T;
+  k.blocks_most = (int32_t)((a->max_tokens + unit - 1) / unit);
   const int64_t blocks = (int64_t)a->n_seqs * k.blocks_most;
   k.layers_wave = (int32_t)std::min<int64_t>(
       layer_count, std::max<int64_t>(1, blocks * layer_count / 8192));
