@@ -42,6 +42,12 @@ __device__ inline void to_lds(uint32_t at, const uint8_t *p) {
                : "s"(at), "v"(p)
                : "memory");
 }
+// A value that has arrived.  The compiler waits for its own loads where their
+// values are used: in the steps' loop it would wait for the rows on their way too.
+template <typename V>
+__device__ inline void here(V &v) {
+  asm volatile("" : "+v"(v));
+}
 template <int N>
 __device__ inline void wait_loads() {
   static_assert(N >= 0 && N < 64, "the counter's range");
@@ -163,6 +169,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   constexpr int KC = CT * EB / 64, KR = EB;   // 16-byte reads of a tile's keys
   constexpr int KS = (CT + kTurn) / 32;       // products of a tile's scores
   constexpr int DT = CT / 32;
+  constexpr int AHEAD = 5, VAHEAD = 4;        // reads of keys, values ahead of their use
   constexpr int VT = DT == 16 ? 1 : 0;        // tiles of O, the last, in vector registers
   constexpr int PV = FP8 ? kF16 : ACT;
   constexpr bool HILO = PV == kBf16 && QW < 4;
@@ -255,10 +262,18 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
       qreg[nb][k] = *reinterpret_cast<const u32x4 *>(p);
     }
   }
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) here(qreg[nb][k]);
   // the row of this lane's column of O^T
   const int my = r0 + qg * 32 + c, my_q = my / HQ;
   const bool mine = my < rows_all;
   const int lim = mine ? min(pos0 + my_q + 1, sq.len) : INT32_MAX;
+
+  // the n-th tile of O that a tile of tokens adds to: that in vector registers
+  // first, which nothing may read until its products are done
+  auto tile_of_sum = [](int n) { return (n + DT - VT) % DT; };
 
   // ---- where tokens lie.  A group's tile n is 16 tokens from tile_at(n) on.
   // Pages of whole tiles: lane l looks up tile n0 + l; else token l % 16 of tile
@@ -272,6 +287,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     const uint32_t pg = table[min(e, last_entry)];
     slot = max(min(tok, end - 1), 0) - e * T;
     page = tok < end && pg < (uint32_t)kv.num_pages ? pg : ~0u;
+    here(page);
+    here(slot);
   };
 
   // ---- loads.  A token's 16-byte pieces lie in LDS in another order for each
@@ -374,6 +391,29 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   int n0_of = -(1 << 20);
   uint64_t gone_of = 0;
 
+  // Sixteen bytes of a token's key; a tile's values, eight tokens of an element.
+  auto key_piece = [&](const uint8_t *tile, int k) {
+    return *reinterpret_cast<const u32x4 *>(
+        tile + (k >= KC ? turn_at[(k - KC) & 1] : key_at[k & 1] + (k >> 1) * 128));
+  };
+  struct Values {
+    u32x2 w[FP8 ? 1 : 2];
+  };
+  auto value_piece = [&](const uint8_t *tile, int dt) {
+    const uint8_t *p = tile + dt / VB * 128;
+    Values v;
+    if constexpr (FP8) {
+      v.w[0] = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p + val_at[dt % VB][0])));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        v.w[j] = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][j])));
+    }
+    return v;
+  };
+
   // Zeros in place of a tile's values that are not finite, once every wave that
   // shares it has read its keys.
   auto mend = [&](int step, int kt) {
@@ -406,6 +446,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
         const float *sp = kv.scales + (uint64_t)(page_of == ~0u ? 0 : page_of) * 2;
         sc_of = page_of == ~0u ? 1.f : sp[0];
         sr_of = page_of == ~0u ? 1.f : sp[1];
+        here(sc_of);
+        here(sr_of);
       }
     }
     // some row attends to a token here that another does not
@@ -418,26 +460,37 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
       f32x4 x[2], xr[2];
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb) x[nb] = xr[nb] = {0.f, 0.f, 0.f, 0.f};
+      u32x4 w[AHEAD + 1];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) w[k] = key_piece(tile, k);
 #pragma unroll
       for (int k = 0; k < KC + KR; ++k) {
-        const bool turn = k >= KC;
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(
-            tile + (turn ? turn_at[(k - KC) & 1] : key_at[k & 1] + (k >> 1) * 128));
+        if (k + AHEAD < KC + KR) w[(k + AHEAD) % (AHEAD + 1)] = key_piece(tile, k + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        const u32x4 v = w[k % (AHEAD + 1)];
         if constexpr (FP8) {
+          f32x4 *to = k >= KC ? xr : x;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1];
-            const u32x4 af = {fp8_pair<ACT, false>(w0), fp8_pair<ACT, true>(w0),
-                              fp8_pair<ACT, false>(w1), fp8_pair<ACT, true>(w1)};
-            f32x4 *to = turn ? xr : x;
+            const u32x4 af = {fp8_pair<ACT, false>(v[2 * j]), fp8_pair<ACT, true>(v[2 * j]),
+                              fp8_pair<ACT, false>(v[2 * j + 1]),
+                              fp8_pair<ACT, true>(v[2 * j + 1])};
             multiply<ACT>(to[0], to[1], af, qreg[0][2 * k + j], qreg[1][2 * k + j]);
           }
         } else {
-          multiply<ACT>(x[0], x[1], w, qreg[0][k], qreg[1][k]);
+          multiply<ACT>(x[0], x[1], v, qreg[0][k], qreg[1][k]);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
       settled(x[0], x[1]);
       if (FP8) settled(xr[0], xr[1]);
+      // Where rows attend to different tokens, values that are not finite count
+      // as zero and are left for the end
+      if (cut) mend(step, kt);
+      Values vw[VAHEAD + 1];
+#pragma unroll
+      for (int n = 0; n < VAHEAD; ++n) vw[n] = value_piece(tile, tile_of_sum(n));
+      __builtin_amdgcn_sched_barrier(0);
       // ---- weights.  Exchanged so that a lane has tokens h * 8 + 0 .. 7 of
       // column c, as the second product takes them
       const int n = step * NT + kt, at_n = n - n0_of, tok0 = tile_at(n);
@@ -525,26 +578,20 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
                                     p[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
         }
       }
-      // ---- O^T += V^T P^T.  Where rows attend to different tokens, values that
-      // are not finite count as zero and are left for the end
-      if (cut) mend(step, kt);
+      // ---- O^T += V^T P^T
 #pragma unroll
       for (int n = 0; n < DT; ++n) {
-        const int dt = (n + DT - VT) % DT;  // the tile in vector registers first
-        const uint8_t *p = tile + dt / VB * 128;
+        const int dt = tile_of_sum(n);
+        if (n + VAHEAD < DT)
+          vw[(n + VAHEAD) % (VAHEAD + 1)] = value_piece(tile, tile_of_sum(n + VAHEAD));
+        __builtin_amdgcn_sched_barrier(0);
+        const Values v = vw[n % (VAHEAD + 1)];
         u32x4 af;
-        if constexpr (FP8) {
-          const i32x2 w =
-              __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p + val_at[dt % VB][0]));
-          af = u32x4{fp8_pair<PV, false>(w[0]), fp8_pair<PV, true>(w[0]),
-                     fp8_pair<PV, false>(w[1]), fp8_pair<PV, true>(w[1])};
-        } else {
-          const u32x2 x0 = __builtin_bit_cast(
-              u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][0])));
-          const u32x2 x1 = __builtin_bit_cast(
-              u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][1])));
-          af = u32x4{x0[0], x0[1], x1[0], x1[1]};
-        }
+        if constexpr (FP8)
+          af = u32x4{fp8_pair<PV, false>(v.w[0][0]), fp8_pair<PV, true>(v.w[0][0]),
+                     fp8_pair<PV, false>(v.w[0][1]), fp8_pair<PV, true>(v.w[0][1])};
+        else
+          af = u32x4{v.w[0][0], v.w[0][1], v.w[1][0], v.w[1][1]};
         if (dt < DT - VT) {
           f32x16 &to = o[dt < DT - VT ? dt : 0];
           to = mfma32<PV>(af, ph, to);
@@ -553,6 +600,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
           multiply32<PV>(ov[0], af, ph);
           if constexpr (HILO) multiply32<PV>(ov[0], af, pl);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
