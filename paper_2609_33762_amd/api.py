@@ -394,7 +394,7 @@ class LatentCache(Cache):
         ref, s = C.byref(a), self._stream(stream)
         need = batch.need(("latent", self._shape, heads), self._lib.ea_attend_latent_workspace,
                           self._h, ref)
-        ws = batch.workspace("attend", need, s)
+        ws = batch.workspace("latent", need, s)
         N.check("ea_attend_latent", self._lib.ea_attend_latent(
             self._h, layer, batch.ref, ref, None if ws is None else ws.data_ptr(), need, s))
 

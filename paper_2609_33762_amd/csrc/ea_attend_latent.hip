@@ -9,7 +9,6 @@
 #include <hip/hip_runtime.h>
 
 #include "ea_kv_device.hpp"
-#include "ea_kv_parts.hpp"
 
 namespace ea {
 namespace {
@@ -183,7 +182,6 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   constexpr int BYTES = NST * STAGE > JOIN ? NST * STAGE : JOIN;
   __shared__ __align__(1024) uint8_t ring[BYTES];
   __shared__ float wave_ml[kWaves][32][2];
-  __shared__ int32_t arrived;
 
   const KvLayer &kv = a.kv;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, c = lane & 31, h = lane >> 5;
@@ -240,8 +238,10 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const int end = max(min(pos0 + q_last + 1, sq.len), 0);
   const int steps = (end + STEP - 1) / STEP, share = steps / parts, more_for = steps % parts;
   const int from = part * share + min(part, more_for);
-  const int n_steps = share + (part < more_for ? 1 : 0);
-  const int p0 = from * STEP;
+  const int part_steps = share + (part < more_for ? 1 : 0), p0 = from * STEP;
+  // the wave's: where it has its tokens to itself it stops at the last one
+  const int n_steps =
+      QW > 1 ? part_steps : min(part_steps, max(0, (end - p0 - kg * 16 + STEP - 1) / STEP));
   const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
   const int last_entry = over_page(kv, max(end - 1, 0));
 
@@ -320,33 +320,51 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
       const uint32_t lat = tile + half * RC, trn = tile + 16 * RC + half * RR;
       const uint32_t pg = __builtin_amdgcn_readlane(load_page, whole ? at_n : at_n * 16);
       const int sl = __builtin_amdgcn_readlane(load_slot, whole ? at_n : at_n * 16);
-      if (full && whole && pg != ~0u && tile_at(n) + 16 <= end) {
-        const uint8_t *base = kv.base + ((uint64_t)pg * (uint32_t)kv.piece +
-                                         (uint32_t)(sl + half) * row_bytes);
+      const int held = end - tile_at(n);  // tokens from the tile's first on
+      if (whole && pg != ~0u) {
+        // (a page outside the cache, or a tile past the end, has pg ~0)
+        const uint8_t *base =
+            kv.base + ((uint64_t)pg * (uint32_t)kv.piece + (uint32_t)sl * row_bytes);
+        if (full && held >= 16) {
+          base += half * row_bytes;
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-          to_lds(lat + i * 1024, base + i * RPI * row_bytes,
-                 (lat_piece ^ (swap_of(i * RPI) << 4)) + lat_row);
-        if (!FP8 || lane < 32) to_lds(trn, base, turn_off);
-      } else {  // tokens that nobody attends to, and pieces past a part, are zeros
+          for (int i = 0; i < NI; ++i)
+            to_lds(lat + i * 1024, base + i * RPI * row_bytes,
+                   (lat_piece ^ (swap_of(i * RPI) << 4)) + lat_row);
+          if (!FP8 || lane < 32) to_lds(trn, base, turn_off);
+        } else {
+          // Past the last token stand copies of it, which nobody attends to.  Of a
+          // token's pieces those past its parts stay the zeros that they were.
+          const int last = min(held, 16) - 1;
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const uint32_t piece = lat_piece ^ (swap_of(i * RPI) << 4);
+            if (piece < (uint32_t)(C * EB))
+              to_lds(lat + i * 1024, base,
+                     piece + min(half + i * RPI + lane / LPR, last) * row_bytes);
+          }
+          if (turn_piece * 16 < R * EB && (!FP8 || lane < 32))
+            to_lds(trn, base,
+                   turn_off + (min(half + turn_row, last) - turn_row) * (int)row_bytes);
+        }
+      } else {
 #pragma unroll 1
         for (int i = 0; i <= NI; ++i) {
           const bool turn = i == NI;
           const int row = turn ? turn_row : i * RPI + lane / LPR;
-          uint32_t page = pg;
-          int slot = sl + half + row;
+          uint32_t page = ~0u;
+          int slot = 0;
           if (!whole) {
             page = __shfl(load_page, at_n * 16 + half + row);
             slot = __shfl(load_slot, at_n * 16 + half + row);
           }
           const int piece = turn ? turn_piece : (lane % LPR) ^ swap_of(row);
-          const bool ok = page != ~0u && tile_at(n) + half + row < end &&
-                          piece * 16 < (turn ? R : C) * EB;
           const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece +
                                         (uint32_t)slot * row_bytes + (turn ? C * EB : 0) +
                                         piece * 16);
-          if (!ok) p = reinterpret_cast<const uint8_t *>(&kZeros);
-          if (!FP8 || !turn || lane < 32) to_lds(turn ? trn : lat + i * 1024, p);
+          if (page == ~0u) p = reinterpret_cast<const uint8_t *>(&kZeros);
+          if (piece * 16 < (turn ? R : C) * EB && (!FP8 || !turn || lane < 32))
+            to_lds(turn ? trn : lat + i * 1024, p);
         }
       }
     }
@@ -605,6 +623,11 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     }
   };
 
+  if (!full) {  // pieces past a token's parts
+    for (int i = threadIdx.x * 16; i < NST * STAGE; i += kThreads * 16)
+      *reinterpret_cast<u32x4 *>(ring + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
   // ---- the ring: steps load NST - 1 ahead of their use
 #pragma unroll 1
   for (int i = 0; i < min(NST - 1, n_steps); ++i) load(i);
@@ -627,7 +650,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   // weight that is not zero made the whole row NaN, zero times them is NaN too
   if (!FP8 && __syncthreads_or(odd != 0)) {
     asm volatile("s_nop 15\n\ts_nop 7" : : : "memory");  // as in rescale()
-    const int last = min(p0 + n_steps * STEP, end);
+    const int last = min(p0 + part_steps * STEP, end);
     for (int at = max(all_lim & ~(STEP - 1), p0); at < last; ++at) {
       const int e = over_page(kv, at);
       const uint32_t page = table[e];
@@ -660,30 +683,36 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     }
   }
 
-  // ---- the groups' sums become one
+  // ---- the groups' sums become one: the rows' output, or a part of it, which
+  // lies as the registers do, [32 rows][tile of 32 elements][i4][lane]
   const float total_of = add_rows32(l);
   const float ref_of = m == kNegInf ? kNegInf : m - kShift;
-  float *part_of = a.parts + (int64_t)blockIdx.x * (QW * 32) * (C + 2);
+  const int cols = (C + 31) & ~31;
+  float *part_of = a.parts + (int64_t)blockIdx.x * (QW * 32) * (cols + 2);
   const int64_t row = sq.row0 + my_q, head = my - my_q * HQ;
   auto emit = [&](int dt, int i4, const f32x4 &v, float norm) {
     const int d = dt * 32 + i4 * 8 + h * 4;
     if (!mine || d >= C) return;
-    if (parts == 1) {
-      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride + d) =
+    if (parts == 1)
+      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride +
+                                 d) =
           u32x2{pack_act<ACT>(v[0] * norm, v[1] * norm), pack_act<ACT>(v[2] * norm, v[3] * norm)};
-    } else {
-      float *op = part_of + (qg * 32 + c) * C + d;
-      put_part(op, v[0], v[1]);
-      put_part(op + 2, v[2], v[3]);
-    }
+    else
+      *reinterpret_cast<f32x4 *>(part_of + qg * 32 * cols +
+                                 ((dt * 4 + i4) * kLanes + lane) * 4) = v;
   };
   auto emit_statistics = [&](float ref, float total) {
     if (!mine || h) return;
-    if (parts > 1) put_part(part_of + QW * 32 * C + 2 * (qg * 32 + c), ref, total);
+    if (parts > 1)
+      *reinterpret_cast<f32x2 *>(part_of + QW * 32 * cols + 2 * (qg * 32 + c)) = f32x2{ref, total};
     else if (a.lse)
       a.lse[row * HQ + head] =
           total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
   };
+  if (a.slices > 0 && part == 0 && threadIdx.x == 0) {  // for the join
+    a.units[2 * ((int64_t)s * a.tiles_most + r0 / (QW * 32))] = blockIdx.x;
+    a.units[2 * ((int64_t)s * a.tiles_most + r0 / (QW * 32)) + 1] = parts;
+  }
   if constexpr (KG == 1) {
     const float norm = total_of == 0.f ? 0.f : 1.f / total_of;
 #pragma unroll
@@ -739,79 +768,68 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     }
     if (kg == 0) emit_statistics(ref, total);
   }
-  if (parts == 1) return;
+}
 
-  // ---- eight parts are joined by the workgroup of them that ends last, then
-  // eight of those, and so on
-  const int w0 = blockIdx.x - part, rows_here = min(QW * 32, rows_all - r0);
-  for (int stride = 1, level = 0;; stride *= kJoin, ++level) {
-    const int at = part / (stride * kJoin) * (stride * kJoin);  // first of the eight
-    const int of = min((parts - at + stride - 1) / stride, kJoin);
-    const bool last = parts <= stride * kJoin;
-    if (of > 1) {
-      if (!last_of(a.arrivals + w0 + at + level, of, &arrived)) return;
-      // o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i, four elements a thread
-      const int quads = C / 4;
-      const int64_t pitch = (int64_t)(QW * 32) * (C + 2);
-      float *p0_of = a.parts + (int64_t)(w0 + at) * pitch;
-      for (int i = threadIdx.x; i < rows_here * quads; i += kThreads) {
-        const int r = i / quads, d = (i - r * quads) * 4;
-        f32x2 ml[kJoin], u[kJoin], v[kJoin];
-#pragma unroll
-        for (int k = 0; k < kJoin; ++k) {
-          const float *p = p0_of + min(k, of - 1) * stride * pitch;
-          ml[k] = get_part(p + QW * 32 * C + 2 * r);
-          u[k] = get_part(p + r * C + d);
-          v[k] = get_part(p + r * C + d + 2);
-        }
-        float ref = kNegInf, total = 0.f;
-#pragma unroll
-        for (int k = 0; k < kJoin; ++k) ref = fmaxf(ref, ml[k][0]);
-        const float zero = ref == kNegInf ? 0.f : ref;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < kJoin; ++k) {
-          if (k < of) {
-            const float f = exp2_fast(ml[k][0] - zero);
-            total += f * ml[k][1];
-            acc += f * f32x4{u[k][0], u[k][1], v[k][0], v[k][1]};
-          }
-        }
-        if (!last) {
-          // the first part's place: its sums were read above by this thread, its
-          // statistics by others too, so they go behind the last row's
-          put_part(p0_of + r * C + d, acc[0], acc[1]);
-          put_part(p0_of + r * C + d + 2, acc[2], acc[3]);
-        } else {
-          const float f = total == 0.f ? 0.f : 1.f / total;
-          const int rr = r0 + r, q = rr / HQ;
-          *reinterpret_cast<u32x2 *>(a.out.data + (sq.row0 + q) * a.out.row_stride +
-                                     (int64_t)(rr - q * HQ) * a.out.head_stride + d) =
-              u32x2{pack_act<ACT>(acc[0] * f, acc[1] * f), pack_act<ACT>(acc[2] * f, acc[3] * f)};
-          if (a.lse && d == 0)
-            a.lse[(int64_t)(sq.row0 + q) * HQ + rr - q * HQ] =
-                total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
-        }
-      }
-      if (!last) {
-        __syncthreads();  // every thread has read the statistics
-        for (int r = threadIdx.x; r < rows_here; r += kThreads) {
-          f32x2 ml[kJoin];
-          float ref = kNegInf, total = 0.f;
-#pragma unroll
-          for (int k = 0; k < kJoin; ++k) {
-            ml[k] = get_part(p0_of + min(k, of - 1) * stride * pitch + QW * 32 * C + 2 * r);
-            ref = fmaxf(ref, ml[k][0]);
-          }
-          const float zero = ref == kNegInf ? 0.f : ref;
-#pragma unroll
-          for (int k = 0; k < kJoin; ++k)
-            if (k < of) total += exp2_fast(ml[k][0] - zero) * ml[k][1];
-          put_part(p0_of + QW * 32 * C + 2 * r, ref, total);
-        }
-      }
+// Joins the parts of a unit's 32 rows, some tiles of 32 elements:
+//   o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i,  m = max_i m_i.
+// A launch of its own, so that many workgroups read the parts and nothing waits
+// or counts.  Wave (g, i4): a quarter of a tile's elements, every kGroups-th part.
+constexpr int kGroups = 4, kJoinThreads = kGroups * 4 * kLanes;
+template <int ACT>
+__global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) {
+  __shared__ f32x4 sums[kGroups][4][kLanes];
+  const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+  const int wave = uniform((int)threadIdx.x >> 6), i4 = wave & 3, g = wave >> 2;
+  const int QW = a.wave_columns, HQ = a.q_heads, C = a.latent, cols = (C + 31) & ~31;
+  uint32_t u = blockIdx.x;
+  const int slice = u % a.slices;
+  u /= a.slices;
+  const int qg = u % QW;
+  u /= QW;
+  const int tile = u % a.tiles_most, s = u / a.tiles_most;
+  const Seq sq = sequence(a.b, s);
+  const int r = tile * QW * 32 + qg * 32 + c, rows_all = sq.rows * HQ;
+  if (r - c >= rows_all) return;
+  const int w0 = a.units[2 * ((int64_t)s * a.tiles_most + tile)];
+  const int parts = a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1];
+  if (parts <= 1) return;
+  const bool mine = r < rows_all;
+  const int64_t pitch = (int64_t)(QW * 32) * (cols + 2);
+  const float *first = a.parts + (int64_t)w0 * pitch;
+  const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);
+  float ref = kNegInf, total = 0.f;
+  if (mine) {
+    for (int k = 0; k < parts; ++k) ref = fmaxf(ref, ml[k * pitch]);
+  }
+  const float zero = ref == kNegInf ? 0.f : ref;
+  if (mine) {
+    for (int k = 0; k < parts; ++k) total += exp2_fast(ml[k * pitch] - zero) * ml[k * pitch + 1];
+  }
+  const float norm = total == 0.f ? 0.f : 1.f / total;
+  const int64_t row = sq.row0 + r / HQ, head = r % HQ;
+  if (mine && slice == 0 && wave == 0 && h == 0 && a.lse)
+    a.lse[row * HQ + head] =
+        total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+  for (int dt = slice; dt < cols / 32; dt += a.slices) {
+    const int d = dt * 32 + i4 * 8 + h * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (mine && d < C) {
+      const float *p = first + qg * 32 * cols + ((dt * 4 + i4) * kLanes + lane) * 4;
+#pragma unroll 4
+      for (int k = g; k < parts; k += kGroups)
+        acc += exp2_fast(ml[k * pitch] - zero) * *reinterpret_cast<const f32x4 *>(p + k * pitch);
     }
-    if (last) return;
+    sums[g][i4][lane] = acc;
+    __syncthreads();
+    if (g == 0 && mine && d < C) {
+#pragma unroll
+      for (int k = 1; k < kGroups; ++k) acc += sums[k][i4][lane];
+      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride +
+                                 d) =
+          u32x2{pack_act<ACT>(acc[0] * norm, acc[1] * norm),
+                pack_act<ACT>(acc[2] * norm, acc[3] * norm)};
+    }
+    __syncthreads();
   }
 }
 
@@ -823,6 +841,10 @@ hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
     case 2: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 2>), grid, block, 0, s, a); break;
     default: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 4>), grid, block, 0, s, a);
   }
+  if (a.slices > 0)
+    hipLaunchKernelGGL(join_latent<ACT>,
+                       dim3((unsigned)a.b.n_seqs * a.tiles_most * a.wave_columns * a.slices),
+                       dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -104,12 +104,15 @@ struct LatentAttendArgs {
   int32_t q_heads;
   float scale_log2;         // softmax scale times log2(e)
   // A workgroup takes 32 * wave_columns (1, 2, 4) rows times heads of a
-  // sequence, a unit; split_wgs, least_steps, split_grid, parts and arrivals are
-  // as for the split kernel.
-  int32_t wave_columns;
+  // sequence, a unit, at most tiles_most of them a sequence.  Units come in parts
+  // so that those of all fit split_wgs workgroups where they can, a part having
+  // least_steps steps at least (0: units are not split); split_grid workgroups
+  // are enough for that.
+  int32_t wave_columns, tiles_most;
   int32_t split_wgs, least_steps, split_grid;
+  int32_t *units;           // [n_seqs][tiles_most][2]: a unit's first workgroup, its parts
   float *parts;             // [split_grid][32 * wave_columns][latent + 2]
-  int32_t *arrivals;
+  int32_t slices;           // workgroups that join a unit's 32 rows; 0: nothing is split
 };
 
 struct LatentAppendArgs {

@@ -16,29 +16,36 @@ using namespace ea::host;
 
 namespace {
 
-// How an attention call is split along its tokens, and its workspace: the
-// counters, always first, then the parts.
-constexpr int64_t kCounters = ea::kArrivals * 4;
+// How an attention call is split along its tokens, and its workspace: where the
+// units' parts are, the parts.
 struct Parts {
-  int32_t wave_columns, wgs, least_steps, grid;
-  int64_t bytes;
+  int32_t wave_columns, tiles, wgs, least_steps, grid, slices;
+  int64_t unit_bytes, bytes;
 };
 
+static int env(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
 Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *a) {
   Parts p{};
   const int64_t most = (int64_t)b->max_rows * a->q_heads;
-  p.wgs = std::min(compute_units(ea::cache_device(c)), ea::kArrivals - ea::kSplitUnits);
+  const int cus = compute_units(ea::cache_device(c));
   p.wave_columns = most <= 32 ? 1 : most <= 64 ? 2 : 4;
+  p.wave_columns = env("EA_QW", p.wave_columns);
   const int64_t tile = 32 * p.wave_columns;
-  const int64_t units =
-      std::min<int64_t>(b->n_seqs * ((most + tile - 1) / tile),
-                        (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
-  p.least_steps = units <= ea::kSplitUnits ? 2 : 0;
+  p.tiles = (int32_t)((most + tile - 1) / tile);
+  const int64_t units = std::min<int64_t>((int64_t)b->n_seqs * p.tiles,
+                                          (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
+  p.wgs = units <= cus ? cus : 2 * cus;
+  p.least_steps = units <= cus ? env("EA_LEAST", 4) : units < p.wgs ? 16 : 0;
   const int64_t step = ea::latent_step(p.wave_columns);
   const int64_t steps = (b->max_kv + step - 1) / step;
   const int64_t whole = p.least_steps ? (steps + p.least_steps - 1) / p.least_steps : 1;
   p.grid = (int32_t)std::min<int64_t>(p.wgs + units, units * whole);
-  if (p.grid > units) p.bytes = kCounters + up((int64_t)p.grid * tile * (a->latent_dim + 2) * 4, 16);
+  if (p.grid > units) {
+    const int64_t groups = (int64_t)b->n_seqs * p.tiles * p.wave_columns;
+    p.slices = (int32_t)std::min<int64_t>(16, std::max<int64_t>(1, 1024 / groups));
+    p.unit_bytes = up((int64_t)b->n_seqs * p.tiles * 8, 16);
+    p.bytes = p.unit_bytes + (int64_t)p.grid * tile * (up(a->latent_dim, 32) + 2) * 4;
+  }
   return p;
 }
 
@@ -126,12 +133,13 @@ int ea_attend_latent(ea_cache *c, int32_t layer, const ea_batch *b, const ea_lat
   k.q_heads = a->q_heads;
   k.scale_log2 = a->scale * 1.4426950408889634f;
   k.wave_columns = p.wave_columns;
+  k.tiles_most = p.tiles;
   k.split_wgs = p.wgs;
   k.least_steps = p.least_steps;
   k.split_grid = p.grid;
-  uint8_t *ws = static_cast<uint8_t *>(workspace);
-  k.arrivals = reinterpret_cast<int32_t *>(ws);
-  k.parts = reinterpret_cast<float *>(ws + kCounters);
+  k.units = static_cast<int32_t *>(workspace);
+  k.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.unit_bytes);
+  k.slices = p.slices;
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());
   KV_HIP(ea::launch_attend_latent(k, a->dtype, ea::cache_desc(c).elem_bytes == 1, stream));
