@@ -18,6 +18,7 @@ typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kLanes;
@@ -26,19 +27,22 @@ constexpr int kRing = 147456;  // most bytes of tokens in LDS
 
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
 
-// 16 bytes a lane from base + off (from p) to LDS, lane by lane from `at` on.
-// The load writes no register, and the compiler does not know of it: whoever
-// reads the bytes waits for it (vmcnt).
-__device__ inline void to_lds(uint32_t at, const uint8_t *base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+// 16 bytes a lane from base + off (from p) to LDS, lane by lane from `at` on, for
+// the lanes in `lanes`.  The load writes no register, and the compiler does not
+// know of it: whoever reads the bytes waits for it (vmcnt).  Every call counts as
+// one load, whatever its lanes.  All lanes are active where these stand.
+__device__ inline void to_lds(uint32_t at, const uint8_t *base, uint32_t off, uint64_t lanes) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\t"
+               "global_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
                :
-               : "s"(at), "v"(off), "s"(base)
+               : "s"(at), "v"(off), "s"(base), "s"(lanes)
                : "memory");
 }
-__device__ inline void to_lds(uint32_t at, const uint8_t *p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+__device__ inline void to_lds(uint32_t at, const uint8_t *p, uint64_t lanes) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\t"
+               "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1"
                :
-               : "s"(at), "v"(p)
+               : "s"(at), "v"(p), "s"(lanes)
                : "memory");
 }
 // A value that has arrived.  The compiler waits for its own loads where their
@@ -137,6 +141,10 @@ __device__ inline void add4(f32x16 &o, int i4, const float (&add)[4]) {
   o[i4 * 4 + 3] = t3;
 }
 
+__device__ inline float of_lane(float v, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+
 struct SeqTiles {
   Seq q;
   int32_t units, steps;
@@ -154,7 +162,7 @@ __device__ inline SeqTiles tiles_of(const LatentAttendArgs &a, int s) {
   return w;
 }
 
-template <int ACT, bool FP8, int CT, int QW>
+template <int ACT, bool FP8, int CT, int QW, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a) {
   constexpr int KG = kWaves / QW;        // groups of waves that share tokens
   constexpr int NT = QW == 4 ? 2 : 1;    // tiles of 16 tokens in a group's step
@@ -167,8 +175,9 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   constexpr int NST = kRing / STAGE < 4 ? kRing / STAGE : 4;  // steps in LDS
   constexpr int KC = CT * EB / 64, KR = EB;   // 16-byte reads of a tile's keys
   constexpr int KS = (CT + kTurn) / 32;       // products of a tile's scores
-  constexpr int DT = CT / 32;
-  constexpr int AHEAD = 5, VAHEAD = 4;        // reads of keys, values ahead of their use
+  constexpr int DT = CT / 32, VB = 8 / EB;    // tiles of O; of them in 16 pieces
+  constexpr int AHEAD = 4, VAHEAD = 3;        // reads of keys, values ahead of their use
+  constexpr bool PIPE = NST > 2;              // the next tile's scores beside this one's weights
   constexpr int VT = DT == 16 ? 1 : 0;        // tiles of O, the last, in vector registers
   constexpr int PV = FP8 ? kF16 : ACT;
   constexpr bool HILO = PV == kBf16 && QW < 4;
@@ -240,8 +249,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const int from = part * share + min(part, more_for);
   const int part_steps = share + (part < more_for ? 1 : 0), p0 = from * STEP;
   // the wave's: where it has its tokens to itself it stops at the last one
-  const int n_steps =
-      QW > 1 ? part_steps : min(part_steps, max(0, (end - p0 - kg * 16 + STEP - 1) / STEP));
+  const int n_steps = uniform(
+      QW > 1 ? part_steps : min(part_steps, max(0, (end - p0 - kg * 16 + STEP - 1) / STEP)));
   const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
   const int last_entry = over_page(kv, max(end - 1, 0));
 
@@ -271,18 +280,18 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const bool mine = my < rows_all;
   const int lim = mine ? min(pos0 + my_q + 1, sq.len) : INT32_MAX;
 
-  // the n-th tile of O that a tile of tokens adds to: that in vector registers
-  // first, which nothing may read until its products are done
-  auto tile_of_sum = [](int n) { return (n + DT - VT) % DT; };
+  // the n-th tile of O that a tile of tokens adds to: the last one, which is in
+  // vector registers, first, as nothing may read it until its products are done;
+  // those whose values lie whole 256 bytes apart one after another
+  auto tile_of_sum = [](int n) { return DT - 1 - (n % (DT / VB) * VB + n / (DT / VB)); };
 
   // ---- where tokens lie.  A group's tile n is 16 tokens from tile_at(n) on.
   // Pages of whole tiles: lane l looks up tile n0 + l; else token l % 16 of tile
   // n0 + l / 16.
-  const bool whole = T % 16 == 0;
-  const int batch = whole ? kLanes : kLanes / 16;
+  constexpr int BATCH = WHOLE ? kLanes : kLanes / 16;
   auto tile_at = [&](int n) { return p0 + (n / NT * KG + kg) * NT * 16 + n % NT * 16; };
   auto look = [&](int n0, uint32_t &page, int &slot) {
-    const int tok = whole ? tile_at(n0 + lane) : tile_at(n0 + (lane >> 4)) + c16;
+    const int tok = WHOLE ? tile_at(n0 + lane) : tile_at(n0 + (lane >> 4)) + c16;
     const int e = over_page(kv, min(tok, max(end - 1, 0)));
     const uint32_t pg = table[min(e, last_entry)];
     slot = max(min(tok, end - 1), 0) - e * T;
@@ -292,81 +301,79 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   };
 
   // ---- loads.  A token's 16-byte pieces lie in LDS in another order for each
-  // of eight tokens, so that reads of one piece of eight tokens (keys), and of
-  // two pieces of four (values), fall on different banks.
-  auto swap_of = [](int row) { return ((row & 3) << 1) | ((row >> 2) & 1); };
+  // of sixteen tokens, so that the pieces that half a wave reads at once fall on
+  // different banks (of 64): one of sixteen tokens (keys), four neighbouring ones
+  // of four or two of eight (values).
+  auto swap_of = [](int row) {
+    return FP8 ? (row & 7) << 1 | row >> 3 : (row & 3) << 2 | row >> 2;
+  };
+  auto turn_swap_of = [](int row) { return FP8 ? row >> 2 : row >> 1; };
   const uint32_t ring_at = uniform((uint32_t)(uintptr_t)(lds_u8 *)ring);
   const bool full = C == CT && R == kTurn;
   constexpr int TL = RR / 16;  // lanes of a token's turned part
-  // swap_of(i * RPI + lane / LPR) is the two's swaps together: their bits differ
-  const uint32_t lat_row = lane / LPR * row_bytes,
-                 lat_piece = ((lane % LPR) ^ swap_of(lane / LPR)) << 4;
-  const int turn_row = (lane / TL) & 7;
-  const int turn_piece = (lane % TL) ^ (FP8 ? (turn_row >> 1) & 3 : swap_of(turn_row));
-  const uint32_t turn_off = turn_row * row_bytes + C * EB + (turn_piece << 4);
+  // (the swap of a sum of rows whose bits differ is the swaps' together)
+  const int lat_row = lane / LPR, turn_row = (lane / TL) & 7;
+  const uint32_t lat_piece = ((lane % LPR) ^ swap_of(lat_row)) << 4,
+                 turn_piece = ((lane % TL) ^ turn_swap_of(turn_row)) << 4;
   uint32_t load_page = ~0u;
   int load_slot = 0, load_n0 = -(1 << 20);
-  auto load = [&](int step) {
-#pragma unroll
-    for (int e = 0; e < EIGHTS; ++e) {
-      const int eight = qg * EIGHTS + e, kt = eight >> 1, half = (eight & 1) * 8;
-      const int n = step * NT + kt;
-      if (n - load_n0 >= batch) {
-        load_n0 = n - n % batch;
-        look(load_n0, load_page, load_slot);
-      }
-      const int at_n = n - load_n0;
-      const uint32_t tile = ring_at + (step % NST) * STAGE + (kg * NT + kt) * TILE;
-      const uint32_t lat = tile + half * RC, trn = tile + 16 * RC + half * RR;
-      const uint32_t pg = __builtin_amdgcn_readlane(load_page, whole ? at_n : at_n * 16);
-      const int sl = __builtin_amdgcn_readlane(load_slot, whole ? at_n : at_n * 16);
-      const int held = end - tile_at(n);  // tokens from the tile's first on
-      if (whole && pg != ~0u) {
-        // (a page outside the cache, or a tile past the end, has pg ~0)
-        const uint8_t *base =
-            kv.base + ((uint64_t)pg * (uint32_t)kv.piece + (uint32_t)sl * row_bytes);
-        if (full && held >= 16) {
-          base += half * row_bytes;
-#pragma unroll
-          for (int i = 0; i < NI; ++i)
-            to_lds(lat + i * 1024, base + i * RPI * row_bytes,
-                   (lat_piece ^ (swap_of(i * RPI) << 4)) + lat_row);
-          if (!FP8 || lane < 32) to_lds(trn, base, turn_off);
-        } else {
-          // Past the last token stand copies of it, which nobody attends to.  Of a
-          // token's pieces those past its parts stay the zeros that they were.
-          const int last = min(held, 16) - 1;
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            const uint32_t piece = lat_piece ^ (swap_of(i * RPI) << 4);
-            if (piece < (uint32_t)(C * EB))
-              to_lds(lat + i * 1024, base,
-                     piece + min(half + i * RPI + lane / LPR, last) * row_bytes);
-          }
-          if (turn_piece * 16 < R * EB && (!FP8 || lane < 32))
-            to_lds(trn, base,
-                   turn_off + (min(half + turn_row, last) - turn_row) * (int)row_bytes);
-        }
-      } else {
-#pragma unroll 1
-        for (int i = 0; i <= NI; ++i) {
-          const bool turn = i == NI;
-          const int row = turn ? turn_row : i * RPI + lane / LPR;
-          uint32_t page = ~0u;
-          int slot = 0;
-          if (!whole) {
-            page = __shfl(load_page, at_n * 16 + half + row);
-            slot = __shfl(load_slot, at_n * 16 + half + row);
-          }
-          const int piece = turn ? turn_piece : (lane % LPR) ^ swap_of(row);
-          const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece +
-                                        (uint32_t)slot * row_bytes + (turn ? C * EB : 0) +
-                                        piece * 16);
-          if (page == ~0u) p = reinterpret_cast<const uint8_t *>(&kZeros);
-          if (piece * 16 < (turn ? R : C) * EB && (!FP8 || !turn || lane < 32))
-            to_lds(turn ? trn : lat + i * 1024, p);
-        }
-      }
+  // Eight tokens that the wave is to load: `from` the first's row (a zero where
+  // there is none), rows up to `last`, which takes the place of those behind it;
+  // nobody attends to these.
+  struct Eight {
+    const uint8_t *from;
+    uint32_t to;  // the tile
+    int half, last, at_n;
+    uint32_t rows;  // all ones, or zero
+    uint32_t lanes;
+  };
+  auto eight_of = [&](int step, int e) {
+    const int eight = qg * EIGHTS + e, n = step * NT + (eight >> 1);
+    if (n - load_n0 >= BATCH) {
+      load_n0 = n - n % BATCH;
+      look(load_n0, load_page, load_slot);
+    }
+    Eight x;
+    x.half = (eight & 1) * 8;
+    x.to = ring_at + (step % NST) * STAGE + (kg * NT + (eight >> 1)) * TILE;
+    x.at_n = n - load_n0;
+    x.lanes = step < n_steps ? ~0u : 0;
+    if constexpr (WHOLE) {
+      const uint32_t page = __builtin_amdgcn_readlane(load_page, x.at_n);
+      const uint32_t slot = __builtin_amdgcn_readlane(load_slot, x.at_n);
+      x.rows = page == ~0u ? 0 : ~0u;
+      x.last = min(max(end - tile_at(n), 1), 16) - 1;
+      x.from = page == ~0u ? reinterpret_cast<const uint8_t *>(&kZeros)
+                           : kv.base + ((uint64_t)page * (uint32_t)kv.piece + slot * row_bytes);
+    }
+    return x;
+  };
+  // the i-th of its loads: tokens' latents, then (NI) their turned parts.  Pieces
+  // past a part stay the zeros that they were.
+  auto load_one = [&](const Eight &x, int i) {
+    const bool turn = i == NI;
+    const uint32_t lds = turn ? x.to + 16 * RC + x.half * RR : x.to + x.half * RC + i * 1024;
+    const int at = turn ? x.half : x.half + i * RPI, row = at + (turn ? turn_row : lat_row);
+    const uint32_t piece =
+        turn ? turn_piece ^ (turn_swap_of(at) << 4) : lat_piece ^ (swap_of(at) << 4);
+    // of all lanes; of half of them: eight tokens' turned parts are 512 bytes in fp8
+    uint32_t low = x.lanes, high = turn && FP8 ? 0 : x.lanes;
+    if (!full) {
+      const uint64_t there = __ballot(piece < (uint32_t)((turn ? R : C) * EB));
+      low &= (uint32_t)there;
+      high &= (uint32_t)(there >> 32);
+    }
+    const uint64_t lanes = (uint64_t)uniform(high) << 32 | uniform(low);
+    if constexpr (WHOLE) {
+      const uint32_t off = __umul24(min(row, x.last), row_bytes) + piece + (turn ? C * EB : 0);
+      to_lds(lds, x.from, off & x.rows, lanes);
+    } else {
+      const uint32_t page = __shfl(load_page, x.at_n * 16 + row);
+      const int slot = __shfl(load_slot, x.at_n * 16 + row);
+      const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece +
+                                    (uint32_t)slot * row_bytes + (turn ? C * EB : 0) + piece);
+      if (page == ~0u) p = reinterpret_cast<const uint8_t *>(&kZeros);
+      to_lds(lds, p, lanes);
     }
   };
 
@@ -380,54 +387,70 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   }
   uint32_t odd = 0;
 
-  // places of this lane's reads in a tile
-  int key_at[2], turn_at[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    key_at[i] = c16 * RC + (((i * 4 + g) ^ swap_of(c16)) << 4);
-    turn_at[i] = 16 * RC + c16 * RR +
-                 ((FP8 ? g ^ ((c16 >> 1) & 3) : (i * 4 + g) ^ swap_of(c16)) << 4);
-  }
-  constexpr int VB = FP8 ? 4 : 2;  // 32-element blocks of 128 bytes
-  int val_at[VB][FP8 ? 1 : 2];
-#pragma unroll
-  for (int i = 0; i < VB; ++i) {
-    if constexpr (FP8) {
-      const int row = h * 8 + (c16 >> 1);
-      val_at[i][0] = row * RC + (((i * 2 + (g & 1)) ^ swap_of(row)) << 4) + (c16 & 1) * 8;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = h * 8 + j * 4 + (c16 >> 2), piece = i * 4 + (g & 1) * 2 + ((c16 >> 1) & 1);
-        val_at[i][j] = row * RC + ((piece ^ swap_of(row)) << 4) + (c16 & 1) * 8;
-      }
-    }
-  }
+  // Places of this lane's reads in a tile: of keys, of turned parts, of values.
+  // Which pieces of sixteen are read turns bits 4 to 7 of the place, which are the
+  // low bits of a piece; tiles and rows are whole 256 bytes (turned parts 64, 128).
+  const uint32_t key_at = c16 * RC + ((g ^ swap_of(c16)) << 4);
+  const uint32_t turn_at =
+      16 * RC + c16 * RR + (((g & (TL - 1)) ^ turn_swap_of(c16)) << 4);
+  const int val_row = h * 8 + (FP8 ? c16 >> 1 : c16 >> 2);
+  const uint32_t val_at =
+      val_row * RC + (c16 & 1) * 8 +
+      (((FP8 ? g & 1 : (g & 1) * 2 + ((c16 >> 1) & 1)) ^ swap_of(val_row)) << 4);
 
-  uint32_t page_of = ~0u;  // of the batch of tiles that is computed
-  float sc_of = 0.f, sr_of = 0.f;
-  int n0_of = -(1 << 20);
+  // Of the batch of tiles that is computed: which pages are not there; the scales
+  // of latents, and times scale_log2 of the scores' two parts; the former's
+  // logarithm, within bounds.
   uint64_t gone_of = 0;
-
-  // Sixteen bytes of a token's key; a tile's values, eight tokens of an element.
-  auto key_piece = [&](const uint8_t *tile, int k) {
-    return *reinterpret_cast<const u32x4 *>(
-        tile + (k >= KC ? turn_at[(k - KC) & 1] : key_at[k & 1] + (k >> 1) * 128));
+  float sc_of = 1.f, sc2_of = 1.f, sr2_of = 1.f, log_of = 0.f;
+  int n0_of = -(1 << 20);
+  auto batch = [&](int step) {
+    if (step * NT - n0_of < BATCH) return;
+    n0_of = step * NT - step * NT % BATCH;
+    uint32_t page;
+    int slot;
+    look(n0_of, page, slot);
+    gone_of = __ballot(page == ~0u);
+    if (FP8) {
+      const float *sp = kv.scales + (uint64_t)(page == ~0u ? 0 : page) * 2;
+      float sc = sp[0], sr = sp[1];
+      here(sc);
+      here(sr);
+      sc_of = page == ~0u ? 1.f : sc;
+      sc2_of = sc_of * a.scale_log2;
+      sr2_of = (page == ~0u ? 1.f : sr) * a.scale_log2;
+      log_of = __log2f(fmaxf(fabsf(sc_of), 0x1p-60f));
+    }
   };
+
+  // The i-th piece of a token's key that is read, and of Q beside it: those whose
+  // places differ by whole 256 bytes one after another.
+  constexpr int KQ = KC / 4;
+  auto key_of = [](int i) { return i < KC ? i % KQ * 4 + i / KQ : i; };
+  auto key_piece = [&](uint32_t tile, int i) {
+    const int k = key_of(i);
+    const uint32_t at = k >= KC ? (tile + turn_at) ^ ((k - KC) << 6)
+                                : ((tile + key_at) ^ ((k & 3) << 6)) + (k >> 2) * 256;
+    return *reinterpret_cast<lds_u32x4 *>(at);
+  };
+  // A tile's values: eight tokens of an element for each of 32.
   struct Values {
     u32x2 w[FP8 ? 1 : 2];
   };
-  auto value_piece = [&](const uint8_t *tile, int dt) {
-    const uint8_t *p = tile + dt / VB * 128;
+  auto value_piece = [&](uint32_t tile, int dt) {
     Values v;
     if constexpr (FP8) {
-      v.w[0] = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p + val_at[dt % VB][0])));
+      const uint32_t at = ((tile + val_at) ^ ((dt & 7) << 5)) + (dt >> 3) * 256;
+      v.w[0] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                             reinterpret_cast<lds_i32x2 *>(at)));
     } else {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        v.w[j] = __builtin_bit_cast(
-            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + val_at[dt % VB][j])));
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t at =
+            ((tile + val_at) ^ ((dt & 3) << 6 | j << 4)) + (dt >> 2) * 256 + j * 4 * RC;
+        v.w[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               reinterpret_cast<lds_s16x4 *>(at)));
+      }
     }
     return v;
   };
@@ -453,196 +476,274 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     else wait_reads();
   };
 
-  auto compute = [&](int step) {
-    const uint8_t *base = ring + (step % NST) * STAGE + kg * NT * TILE;
-    if (step * NT - n0_of >= batch) {
-      n0_of = step * NT - step * NT % batch;
-      int slot;
-      look(n0_of, page_of, slot);
-      gone_of = __ballot(page_of == ~0u);
-      if (FP8) {
-        const float *sp = kv.scales + (uint64_t)(page_of == ~0u ? 0 : page_of) * 2;
-        sc_of = page_of == ~0u ? 1.f : sp[0];
-        sr_of = page_of == ~0u ? 1.f : sp[1];
-        here(sc_of);
-        here(sr_of);
-      }
+  // ---- a tile's scores, S^T = K Q^T: columns c16 of two sixteens, tokens
+  // g * 4 + i; beside each read's products something else, side(k)
+  f32x4 x[2], xr[2];
+  auto scores = [&](uint32_t tile, auto before, auto side) {
+    u32x4 w[AHEAD + 1];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) w[k] = key_piece(tile, k);
+    __builtin_amdgcn_sched_barrier(0);
+    before();
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      x[nb] = {0.f, 0.f, 0.f, 0.f};
+      if (FP8) xr[nb] = {0.f, 0.f, 0.f, 0.f};
     }
-    // some row attends to a token here that another does not
-    const int first = p0 + step * STEP;
-    const bool cut = all_lim < end && first + STEP > all_lim;
 #pragma unroll
-    for (int kt = 0; kt < NT; ++kt) {
-      const uint8_t *tile = base + kt * TILE;
-      // ---- scores, S^T = K Q^T: columns c16 of two sixteens, tokens g * 4 + i
-      f32x4 x[2], xr[2];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb) x[nb] = xr[nb] = {0.f, 0.f, 0.f, 0.f};
-      u32x4 w[AHEAD + 1];
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) w[k] = key_piece(tile, k);
-#pragma unroll
-      for (int k = 0; k < KC + KR; ++k) {
-        if (k + AHEAD < KC + KR) w[(k + AHEAD) % (AHEAD + 1)] = key_piece(tile, k + AHEAD);
-        __builtin_amdgcn_sched_barrier(0);
-        const u32x4 v = w[k % (AHEAD + 1)];
-        if constexpr (FP8) {
-          f32x4 *to = k >= KC ? xr : x;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const u32x4 af = {fp8_pair<ACT, false>(v[2 * j]), fp8_pair<ACT, true>(v[2 * j]),
-                              fp8_pair<ACT, false>(v[2 * j + 1]),
-                              fp8_pair<ACT, true>(v[2 * j + 1])};
-            multiply<ACT>(to[0], to[1], af, qreg[0][2 * k + j], qreg[1][2 * k + j]);
-          }
-        } else {
-          multiply<ACT>(x[0], x[1], v, qreg[0][k], qreg[1][k]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      settled(x[0], x[1]);
-      if (FP8) settled(xr[0], xr[1]);
-      // Where rows attend to different tokens, values that are not finite count
-      // as zero and are left for the end
-      if (cut) mend(step, kt);
-      Values vw[VAHEAD + 1];
-#pragma unroll
-      for (int n = 0; n < VAHEAD; ++n) vw[n] = value_piece(tile, tile_of_sum(n));
+    for (int k = 0; k < KC + KR; ++k) {
+      if (k + AHEAD < KC + KR) w[(k + AHEAD) % (AHEAD + 1)] = key_piece(tile, k + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
-      // ---- weights.  Exchanged so that a lane has tokens h * 8 + 0 .. 7 of
-      // column c, as the second product takes them
-      const int n = step * NT + kt, at_n = n - n0_of, tok0 = tile_at(n);
-      float y[8], vs[8], sc[4], sr[4];
+      const u32x4 v = w[k % (AHEAD + 1)];
       if constexpr (FP8) {
-        if (whole) {
-          const float u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc_of), at_n));
-          const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sr_of), at_n));
+        f32x4 *to = k >= KC ? xr : x;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) vs[i] = u;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc[i] = u;
-            sr[i] = v;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc[i] = __shfl(sc_of, at_n * 16 + g * 4 + i);
-            sr[i] = __shfl(sr_of, at_n * 16 + g * 4 + i);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) vs[i] = __shfl(sc_of, at_n * 16 + h * 8 + i);
+        for (int j = 0; j < 2; ++j) {
+          const u32x4 af = {fp8_pair<ACT, false>(v[2 * j]), fp8_pair<ACT, true>(v[2 * j]),
+                            fp8_pair<ACT, false>(v[2 * j + 1]),
+                            fp8_pair<ACT, true>(v[2 * j + 1])};
+          multiply<ACT>(to[0], to[1], af, qreg[0][2 * key_of(k) + j], qreg[1][2 * key_of(k) + j]);
         }
+      } else {
+        multiply<ACT>(x[0], x[1], v, qreg[0][key_of(k)], qreg[1][key_of(k)]);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float u = x[0][i], v = x[1][i];
-        if constexpr (FP8) {
-          u = u * sc[i] + xr[0][i] * sr[i];
-          v = v * sc[i] + xr[1][i] * sr[i];
-        }
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v),
-                                                        false, false);
-        y[i] = __uint_as_float(r[0]) * a.scale_log2;
-        y[4 + i] = __uint_as_float(r[1]) * a.scale_log2;
-      }
-      const uint32_t gone = whole ? ((gone_of >> at_n) & 1 ? 0xffffu : 0u)
-                                  : (uint32_t)(gone_of >> (at_n * 16)) & 0xffffu;
-      if (gone || tok0 + 16 > all_lim) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (tok0 + h * 8 + i >= lim || ((gone >> (h * 8 + i)) & 1)) {
-            y[i] = kNegInf;
-            if (FP8) vs[i] = 0.f;
-          }
-      }
-      // the reference counts a value's scale in, within bounds, so that its
-      // weight with the scale fits 16 bits
-      float top = kNegInf;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float v = y[i];
-        if constexpr (FP8) v += __log2f(fmaxf(fabsf(vs[i]), 0x1p-60f));
-        top = fmaxf(top, v);
-      }
-      top = max_rows32(top);
-      if (__any(top > m + kSlack)) {
-        const float to = top > m + kSlack ? top : m;
-        const float f = m == kNegInf ? 0.f : exp2_fast(m - to);
-        l *= f;
-        rescale(o, f);
-        if (VT) {
-          settled(ov[0]);
-          ov[0] *= f;
-        }
-        m = to;
-      }
-      const float ref = m == kNegInf ? 0.f : m - kShift;
-      u32x4 ph, pl;
-      {
-        float p[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = exp2_fast(y[i] - ref);
-          l += p[i];
-          if (FP8) p[i] *= vs[i];
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t hi = pack_act<PV>(p[2 * w], p[2 * w + 1]);
-          ph[w] = hi;
-          if constexpr (HILO)
-            pl[w] = pack_act<kBf16>(p[2 * w] - __uint_as_float(hi << 16),
-                                    p[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
-        }
-      }
-      // ---- O^T += V^T P^T
-#pragma unroll
-      for (int n = 0; n < DT; ++n) {
-        const int dt = tile_of_sum(n);
-        if (n + VAHEAD < DT)
-          vw[(n + VAHEAD) % (VAHEAD + 1)] = value_piece(tile, tile_of_sum(n + VAHEAD));
-        __builtin_amdgcn_sched_barrier(0);
-        const Values v = vw[n % (VAHEAD + 1)];
-        u32x4 af;
-        if constexpr (FP8)
-          af = u32x4{fp8_pair<PV, false>(v.w[0][0]), fp8_pair<PV, true>(v.w[0][0]),
-                     fp8_pair<PV, false>(v.w[0][1]), fp8_pair<PV, true>(v.w[0][1])};
-        else
-          af = u32x4{v.w[0][0], v.w[0][1], v.w[1][0], v.w[1][1]};
-        if (dt < DT - VT) {
-          f32x16 &to = o[dt < DT - VT ? dt : 0];
-          to = mfma32<PV>(af, ph, to);
-          if constexpr (HILO) to = mfma32<PV>(af, pl, to);
-        } else {
-          multiply32<PV>(ov[0], af, ph);
-          if constexpr (HILO) multiply32<PV>(ov[0], af, pl);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      side(k);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
+  // ---- its weights: scores exchanged so that a lane has tokens h * 8 + 0 .. 7 of
+  // column c, as the second product takes them, masked
+  float y[8], vs[FP8 ? 8 : 1], ls = 0.f;
+  auto exchange = [&](int n) {
+    settled(x[0], x[1]);
+    if (FP8) settled(xr[0], xr[1]);
+    const int at_n = n - n0_of, tok0 = tile_at(n);
+    float sc[4], sr[4];
+    if constexpr (FP8 && WHOLE) {
+      sc[0] = of_lane(sc2_of, at_n);
+      sr[0] = of_lane(sr2_of, at_n);
+      vs[0] = of_lane(sc_of, at_n);
+      ls = of_lane(log_of, at_n);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) vs[i] = vs[0];
+#pragma unroll
+      for (int i = 1; i < 4; ++i) {
+        sc[i] = sc[0];
+        sr[i] = sr[0];
+      }
+    } else if constexpr (FP8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[i] = __shfl(sc2_of, at_n * 16 + g * 4 + i);
+        sr[i] = __shfl(sr2_of, at_n * 16 + g * 4 + i);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vs[i] = __shfl(sc_of, at_n * 16 + h * 8 + i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float u = x[0][i], v = x[1][i];
+      if constexpr (FP8) {
+        u = u * sc[i] + xr[0][i] * sr[i];
+        v = v * sc[i] + xr[1][i] * sr[i];
+      } else {
+        u *= a.scale_log2;
+        v *= a.scale_log2;
+      }
+      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v),
+                                                      false, false);
+      y[i] = __uint_as_float(r[0]);
+      y[4 + i] = __uint_as_float(r[1]);
+    }
+    const uint32_t gone = WHOLE ? ((gone_of >> at_n) & 1 ? 0xffffu : 0u)
+                                : (uint32_t)(gone_of >> (at_n * 16)) & 0xffffu;
+    if (gone || tok0 + 16 > all_lim) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool out = tok0 + h * 8 + i >= lim || ((gone >> (h * 8 + i)) & 1);
+        y[i] = out ? kNegInf : y[i];
+        // (a scale that is not finite, or one of a block that the row sees
+        // nothing of)
+        if (FP8) vs[i] = out ? 0.f : vs[i];
+      }
+    }
+  };
+  // The weights in kSides pieces of about the same work, to stand between
+  // products.  The reference counts a value's scale in, within bounds, so that its
+  // weight with the scale fits 16 bits.
+  constexpr int kSides = 16;
+  float top, f, ref;
+  uint64_t jump = 0;
+  u32x4 ph, pl;
+  auto weigh = [&](int i) {
+    if (i == 0) {
+      if constexpr (FP8 && !WHOLE) {
+        top = kNegInf;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          top = fmaxf(top, y[j] + __log2f(fmaxf(fabsf(vs[j]), 0x1p-60f)));
+      } else {
+        top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])),
+                    fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+      }
+    } else if (i == 1) {
+      if constexpr (FP8 && WHOLE) top += ls;
+      top = max_rows32(top);
+    } else if (i == 2) {
+      const bool over = top > m + kSlack;
+      jump = __ballot(over);
+      top = over ? top : m;
+      f = m == kNegInf ? 0.f : exp2_fast(m - top);
+    } else if (i == 3) {
+      l *= f;
+      m = top;
+      ref = m == kNegInf ? 0.f : m - kShift;
+    } else if (i < 12) {
+      float &p = y[i - 4];
+      p = exp2_fast(p - ref);
+      l += p;
+      if constexpr (FP8) p *= vs[i - 4];
+    } else {
+      const int w = i - 12;
+      const uint32_t hi = pack_act<PV>(y[2 * w], y[2 * w + 1]);
+      ph[w] = hi;
+      if constexpr (HILO)
+        pl[w] = pack_act<kBf16>(y[2 * w] - __uint_as_float(hi << 16),
+                                y[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
+    }
+  };
+  // ---- O^T += V^T P^T, loads of later tokens between the products
+  Values vw[VAHEAD + 1];
+  auto add_values = [&](uint32_t tile, auto side) {
+    if (jump) {
+      rescale(o, f);
+      if (VT) {
+        settled(ov[0]);
+        ov[0] *= f;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < DT; ++n) {
+      const int dt = tile_of_sum(n);
+      if (n + VAHEAD < DT)
+        vw[(n + VAHEAD) % (VAHEAD + 1)] = value_piece(tile, tile_of_sum(n + VAHEAD));
+      __builtin_amdgcn_sched_barrier(0);
+      const Values v = vw[n % (VAHEAD + 1)];
+      u32x4 af;
+      if constexpr (FP8)
+        af = u32x4{fp8_pair<PV, false>(v.w[0][0]), fp8_pair<PV, true>(v.w[0][0]),
+                   fp8_pair<PV, false>(v.w[0][1]), fp8_pair<PV, true>(v.w[0][1])};
+      else
+        af = u32x4{v.w[0][0], v.w[0][1], v.w[1][0], v.w[1][1]};
+      if (dt < DT - VT) {
+        f32x16 &to = o[dt < DT - VT ? dt : 0];
+        to = mfma32<PV>(af, ph, to);
+        if constexpr (HILO) to = mfma32<PV>(af, pl, to);
+      } else {
+        multiply32<PV>(ov[0], af, ph);
+        if constexpr (HILO) multiply32<PV>(ov[0], af, pl);
+      }
+      side(n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // ---- the ring: loads are NST - 1 steps ahead, issued between products.  The
+  // scores of a tile are made beside the weights of the one before it, where there
+  // is room for three steps.  Steps past the last
+  // load nothing, and what is made of their tokens goes unused.
   if (!full) {  // pieces past a token's parts
     for (int i = threadIdx.x * 16; i < NST * STAGE; i += kThreads * 16)
       *reinterpret_cast<u32x4 *>(ring + i) = u32x4{0, 0, 0, 0};
     __syncthreads();
   }
-  // ---- the ring: steps load NST - 1 ahead of their use
+  auto tile_of = [&](int step, int kt) {
+    return ring_at + (step % NST) * STAGE + (kg * NT + kt) * TILE;
+  };
+  auto nothing = [](int) {};
+  constexpr int FIRST = PIPE ? NST - 1 : NST;  // steps that load before the first
+  if (n_steps > 0) {
+    batch(0);
 #pragma unroll 1
-  for (int i = 0; i < min(NST - 1, n_steps); ++i) load(i);
-#pragma unroll 1
-  for (int step = 0; step < n_steps; ++step) {
-    const int behind = min(n_steps - 1 - step, NST - 2);  // later steps on their way
-    if (NST > 3 && behind == 2) wait_loads<(NST > 3 ? 2 : 0) * LOADS>();
-    else if (NST > 2 && behind == 1) wait_loads<(NST > 2 ? 1 : 0) * LOADS>();
-    else wait_loads<0>();
-    wait_reads();
+    for (int step = 0; step < FIRST; ++step)
+#pragma unroll
+      for (int e = 0; e < EIGHTS; ++e) {
+        const Eight from = eight_of(step, e);
+#pragma unroll
+        for (int i = 0; i <= NI; ++i) load_one(from, i);
+      }
+    wait_loads<(FIRST - 1) * LOADS>();
     if (QW > 1) __syncthreads();
-    if (step + NST - 1 < n_steps) load(step + NST - 1);
-    compute(step);
+    scores(tile_of(0, 0), [] {}, nothing);
+#pragma unroll 1
+    for (int step = 0; step < n_steps; ++step) {
+      batch(step);
+      // some row attends to a token here that another does not
+      const int first = p0 + step * STEP;
+      const bool cut = all_lim < end && first + STEP > all_lim;
+      Eight from[EIGHTS];
+      auto load_next = [&](int i) {  // of the step's loads
+        if (i < LOADS) load_one(from[i / (NI + 1)], i % (NI + 1));
+      };
+#pragma unroll
+      for (int kt = 0; kt < NT; ++kt) {
+        const uint32_t tile = tile_of(step, kt);
+        const bool last = kt == NT - 1;
+        // Where rows attend to different tokens, values that are not finite count
+        // as zero and are left for the end
+        if (cut) mend(step, kt);
+        constexpr int EACH = (kSides + KC + KR - 1) / (KC + KR);
+        constexpr int LEACH = (LOADS + DT - 1) / DT, KEACH = (LOADS + KC + KR - 1) / (KC + KR);
+        auto value_ahead = [&](int k) {
+          const int n = k - (KC + KR - VAHEAD);
+          if (n >= 0) vw[n] = value_piece(tile, tile_of_sum(n));
+        };
+        if constexpr (PIPE) {
+          if (last) {
+            wait_loads<(NST - 3) * LOADS>();
+            wait_reads();
+            if (QW > 1) __syncthreads();
+#pragma unroll
+            for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + NST - 1, e);
+          }
+          scores(last ? tile_of(step + 1, 0) : tile_of(step, kt + 1),
+                 [&] { exchange(step * NT + kt); },
+                 [&](int k) {
+#pragma unroll
+                   for (int i = 0; i < EACH; ++i)
+                     if (k * EACH + i < kSides) weigh(k * EACH + i);
+                   value_ahead(k);
+                 });
+          add_values(tile, [&](int n) {
+#pragma unroll
+            for (int i = 0; i < LEACH; ++i)
+              if (last) load_next(n * LEACH + i);
+          });
+        } else {
+          exchange(step);
+#pragma unroll
+          for (int n = 0; n < VAHEAD; ++n) vw[n] = value_piece(tile, tile_of_sum(n));
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < kSides; ++i) weigh(i);
+          add_values(tile, nothing);
+          wait_loads<0>();
+          wait_reads();
+          if (QW > 1) __syncthreads();
+#pragma unroll
+          for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + NST, e);
+          scores(tile_of(step + 1, 0), [] {},
+                 [&](int k) {
+#pragma unroll
+                   for (int i = 0; i < KEACH; ++i) load_next(k * KEACH + i);
+                 });
+        }
+      }
+    }
+    wait_loads<0>();
   }
-
   if (VT) settled(ov[0]);
   auto sum_at = [&](int dt, int i) { return dt < DT - VT ? o[dt < DT - VT ? dt : 0][i] : ov[0][i]; };
 
@@ -833,13 +934,16 @@ __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) 
   }
 }
 
-template <int ACT, bool FP8, int CT>
+void go(void (*kernel)(LatentAttendArgs), const LatentAttendArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.split_grid), dim3(kThreads), 0, s, a);
+}
+
+template <int ACT, bool FP8, int CT, bool WHOLE>
 hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)a.split_grid), block(kThreads);
   switch (a.wave_columns) {
-    case 1: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 1>), grid, block, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 2>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((attend_latent<ACT, FP8, CT, 4>), grid, block, 0, s, a);
+    case 1: go(attend_latent<ACT, FP8, CT, 1, WHOLE>, a, s); break;
+    case 2: go(attend_latent<ACT, FP8, CT, 2, WHOLE>, a, s); break;
+    default: go(attend_latent<ACT, FP8, CT, 4, WHOLE>, a, s);
   }
   if (a.slices > 0)
     hipLaunchKernelGGL(join_latent<ACT>,
@@ -850,8 +954,11 @@ hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
 
 template <int ACT, bool FP8>
 hipError_t latents(const LatentAttendArgs &a, hipStream_t s) {
-  if (a.latent <= 256) return columns<ACT, FP8, 256>(a, s);
-  return columns<ACT, FP8, 512>(a, s);
+  if (a.kv.page_tokens % 16 == 0)
+    return a.latent <= 256 ? columns<ACT, FP8, 256, true>(a, s)
+                           : columns<ACT, FP8, 512, true>(a, s);
+  return a.latent <= 256 ? columns<ACT, FP8, 256, false>(a, s)
+                         : columns<ACT, FP8, 512, false>(a, s);
 }
 
 }  // namespace
