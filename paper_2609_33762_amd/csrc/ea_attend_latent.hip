@@ -27,23 +27,26 @@ constexpr int kRing = 147456;  // most bytes of tokens in LDS
 
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
 
-// 16 bytes a lane from base + off (from p) to LDS, lane by lane from `at` on, for
-// the lanes in `lanes`.  The load writes no register, and the compiler does not
-// know of it: whoever reads the bytes waits for it (vmcnt).  Every call counts as
-// one load, whatever its lanes.  All lanes are active where these stand.
-__device__ inline void to_lds(uint32_t at, const uint8_t *base, uint32_t off, uint64_t lanes) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\t"
-               "global_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+// 16 bytes a lane from base + off (from p) to LDS, lane by lane from `at` on, if
+// `there` is not zero; of the lanes in `lanes`.  The load writes no register, and
+// the compiler does not know of it: whoever reads the bytes waits for it (vmcnt).
+// All lanes are active where these stand.  (Changing them takes as long as the
+// products before it, so that only what needs it does.)
+__device__ inline void to_lds(uint32_t at, const uint8_t *base, uint32_t off, uint32_t there) {
+  asm volatile("s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lpast%=\n\ts_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n.Lpast%=:"
                :
-               : "s"(at), "v"(off), "s"(base), "s"(lanes)
-               : "memory");
+               : "s"(uniform(at)), "v"(off), "s"(base), "s"(uniform(there))
+               : "memory", "scc");
 }
-__device__ inline void to_lds(uint32_t at, const uint8_t *p, uint64_t lanes) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\t"
-               "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1"
+__device__ inline void to_lds_some(uint32_t at, const uint8_t *p, uint32_t there,
+                                   uint64_t lanes) {
+  asm volatile("s_cmp_eq_u32 %2, 0\n\ts_cbranch_scc1 .Lpast%=\n\ts_mov_b32 m0, %0\n\t"
+               "s_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, off\n\t"
+               "s_mov_b64 exec, -1\n.Lpast%=:"
                :
-               : "s"(at), "v"(p), "s"(lanes)
-               : "memory");
+               : "s"(uniform(at)), "v"(p), "s"(uniform(there)), "s"(lanes)
+               : "memory", "scc");
 }
 // A value that has arrived.  The compiler waits for its own loads where their
 // values are used: in the steps' loop it would wait for the rows on their way too.
@@ -58,41 +61,24 @@ __device__ inline void wait_loads() {
 }
 __device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
-// Products of two tiles of columns with the same tokens, into vector registers:
-// the sums of O take all accumulation registers, and the compiler puts results
-// of its own matrix instructions there.  It does not know what these are, so
-// they bring the waits that the hardware asks for: two cycles after a vector
-// instruction has written an operand, eight before one reads the results
-// (settled()).
-template <int ACT>
-__device__ inline void multiply(f32x4 &x0, f32x4 &x1, const u32x4 &w, const u32x4 &q0,
-                                const u32x4 &q1) {
-  if constexpr (ACT == kBf16)
-    asm("s_nop 1\n\t"
-        "v_mfma_f32_16x16x32_bf16 %0, %2, %3, %0\n\t"
-        "v_mfma_f32_16x16x32_bf16 %1, %2, %4, %1"
-        : "+v"(x0), "+v"(x1)
-        : "v"(w), "v"(q0), "v"(q1));
+// A product into vector registers: the sums of O take the accumulation
+// registers, and the compiler puts results of its own matrix instructions there.
+// It does not know what these are, so they bring the waits that the hardware asks
+// for: NOP two cycles after a vector instruction has written an operand, sixteen
+// before one reads the results (settled()).  ZERO: not added to anything.
+template <int ACT, bool ZERO, bool NOP>
+__device__ inline void multiply32(f32x16 &x, const u32x4 &v, const u32x4 &w) {
+  if constexpr (NOP) asm volatile("s_nop 1");
+  if constexpr (ACT == kBf16 && ZERO)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
+  else if constexpr (ACT == kBf16)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
+  else if constexpr (ZERO)
+    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
   else
-    asm("s_nop 1\n\t"
-        "v_mfma_f32_16x16x32_f16 %0, %2, %3, %0\n\t"
-        "v_mfma_f32_16x16x32_f16 %1, %2, %4, %1"
-        : "+v"(x0), "+v"(x1)
-        : "v"(w), "v"(q0), "v"(q1));
+    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
 }
-__device__ inline void settled(f32x4 &x0, f32x4 &x1) {
-  asm("s_nop 9" : "+v"(x0), "+v"(x1));
-}
-
-// The same for a tile of O whose sums are in vector registers.
-template <int ACT>
-__device__ inline void multiply32(f32x16 &o, const u32x4 &v, const u32x4 &p) {
-  if constexpr (ACT == kBf16)
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
-  else
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
-}
-__device__ inline void settled(f32x16 &o) { asm("s_nop 15" : "+v"(o)); }
+__device__ inline void settled(f32x16 &x) { asm volatile("s_nop 15" : "+v"(x)); }
 
 // Sums times f, in their accumulation registers.  Rare, so it waits for any
 // matrix instruction before and behind it.
@@ -162,31 +148,33 @@ __device__ inline SeqTiles tiles_of(const LatentAttendArgs &a, int s) {
   return w;
 }
 
-template <int ACT, bool FP8, int CT, int QW, bool WHOLE>
+// Pages and rows: runs of 16 tokens inside pages and whole rows that the
+// registers hold (kPlain), other rows (kRows), other pages (kPages).
+enum Mode { kPlain, kRows, kPages };
+
+template <int ACT, bool FP8, int CT, int QW, Mode MODE>
 __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a) {
   constexpr int KG = kWaves / QW;        // groups of waves that share tokens
-  constexpr int NT = QW == 4 ? 2 : 1;    // tiles of 16 tokens in a group's step
-  constexpr int STEP = KG * NT * 16;     // tokens of a step
+  constexpr int STEP = KG * 32;          // tokens of a step, 32 a group
   static_assert(STEP == latent_step(QW), "the host counts the same steps");
+  constexpr bool WHOLE = MODE != kPages;
   constexpr int EB = FP8 ? 1 : 2;
   constexpr int RC = CT * EB, RR = kTurn * EB;  // bytes of a token's parts in LDS
-  constexpr int TILE = 16 * (RC + RR);
-  constexpr int STAGE = KG * NT * TILE;
+  constexpr int TILE = 32 * (RC + RR), STAGE = KG * TILE;
   constexpr int NST = kRing / STAGE < 4 ? kRing / STAGE : 4;  // steps in LDS
-  constexpr int KC = CT * EB / 64, KR = EB;   // 16-byte reads of a tile's keys
-  constexpr int KS = (CT + kTurn) / 32;       // products of a tile's scores
-  constexpr int DT = CT / 32, VB = 8 / EB;    // tiles of O; of them in 16 pieces
-  constexpr int AHEAD = 4, VAHEAD = 3;        // reads of keys, values ahead of their use
-  constexpr bool PIPE = NST > 2;              // the next tile's scores beside this one's weights
-  constexpr int VT = DT == 16 ? 1 : 0;        // tiles of O, the last, in vector registers
+  constexpr bool PIPE = NST > 2;         // the next tile's scores beside this one's weights
+  constexpr int KC = RC / 32, KR = RR / 32, KN = KC + KR;  // 16-byte reads of a tile's keys
+  constexpr int KS = (CT + kTurn) / 16;  // products of a tile's scores
+  constexpr int DT = CT / 32, VB = 8 / EB;      // tiles of O; of them in 16 pieces
+  constexpr int AHEAD = 4, VAHEAD = 3;   // reads of keys, values ahead of their use
   constexpr int PV = FP8 ? kF16 : ACT;
   constexpr bool HILO = PV == kBf16 && QW < 4;
   constexpr float kShift = PV == kF16 ? 7.f : 0.f, kSlack = 8.f;
   constexpr int LPR = RC / 16, RPI = kLanes / LPR, NI = 8 / RPI;  // loads of 8 tokens' latents
-  constexpr int EIGHTS = NT * 2 / QW;         // eights of tokens that a wave loads in a step
+  constexpr int EIGHTS = 4 / QW;         // eights of tokens that a wave loads in a step
   constexpr int LOADS = EIGHTS * (NI + 1);
-  static_assert(NST >= 2 && LOADS * (NST - 2) < 64 && EIGHTS >= 1, "shape of the ring");
-  constexpr int CR = CT / 2;                  // elements of a round of the waves' join
+  static_assert(NST >= 2 && LOADS * (NST > 2 ? NST - 2 : 1) < 64, "shape of the ring");
+  constexpr int CR = CT / 2;             // elements of a round of the waves' join
   constexpr int JOIN = KG > 1 ? kWaves * 32 * CR * 4 : 0;
   constexpr int BYTES = NST * STAGE > JOIN ? NST * STAGE : JOIN;
   __shared__ __align__(1024) uint8_t ring[BYTES];
@@ -250,48 +238,41 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const int part_steps = share + (part < more_for ? 1 : 0), p0 = from * STEP;
   // the wave's: where it has its tokens to itself it stops at the last one
   const int n_steps = uniform(
-      QW > 1 ? part_steps : min(part_steps, max(0, (end - p0 - kg * 16 + STEP - 1) / STEP)));
+      QW > 1 ? part_steps : min(part_steps, max(0, (end - p0 - kg * 32 + STEP - 1) / STEP)));
   const int32_t *table = a.b.page_table + (int64_t)s * a.b.table_stride;
   const int last_entry = over_page(kv, max(end - 1, 0));
 
-  // ---- queries: the second operand of S = K Q^T for columns c16 of 16
-  u32x4 qreg[2][KS];
-#pragma unroll
-  for (int nb = 0; nb < 2; ++nb) {
-    const int r = r0 + qg * 32 + nb * 16 + c16, qi = r / HQ;
-    const bool there = r < rows_all;
-    const uint16_t *qp = a.q.data + (int64_t)(sq.row0 + (there ? qi : 0)) * a.q.row_stride +
-                         (int64_t)(there ? r - qi * HQ : 0) * a.q.head_stride;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const int d = FP8 ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
-      const bool in = d < CT ? d < C : d - CT < R;
-      const uint16_t *p = qp + (d < CT ? d : C + d - CT);
-      if (!there || !in) p = reinterpret_cast<const uint16_t *>(&kZeros);
-      qreg[nb][k] = *reinterpret_cast<const u32x4 *>(p);
-    }
-  }
-#pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-    for (int k = 0; k < KS; ++k) here(qreg[nb][k]);
-  // the row of this lane's column of O^T
+  // ---- queries, the second operand of S = K Q^T: column c
   const int my = r0 + qg * 32 + c, my_q = my / HQ;
   const bool mine = my < rows_all;
+  u32x4 qreg[KS];
+  {
+    const uint16_t *qp = a.q.data + (int64_t)(sq.row0 + (mine ? my_q : 0)) * a.q.row_stride +
+                         (int64_t)(mine ? my - my_q * HQ : 0) * a.q.head_stride;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int d = FP8 ? (k >> 1) * 32 + h * 16 + (k & 1) * 8 : k * 16 + h * 8;
+      const bool in = mine && (d < CT ? d < C : d - CT < R);
+      const uint16_t *p = qp + (d < CT ? d : C + d - CT);
+      qreg[k] = *reinterpret_cast<const u32x4 *>(
+          in ? p : reinterpret_cast<const uint16_t *>(&kZeros));
+    }
+#pragma unroll
+    for (int k = 0; k < KS; ++k) here(qreg[k]);
+  }
   const int lim = mine ? min(pos0 + my_q + 1, sq.len) : INT32_MAX;
 
-  // the n-th tile of O that a tile of tokens adds to: the last one, which is in
-  // vector registers, first, as nothing may read it until its products are done;
-  // those whose values lie whole 256 bytes apart one after another
-  auto tile_of_sum = [](int n) { return DT - 1 - (n % (DT / VB) * VB + n / (DT / VB)); };
+  // the n-th tile of O that sixteen tokens add to: those whose values lie whole
+  // 256 bytes apart one after another
+  auto tile_of_sum = [](int n) { return n % (DT / VB) * VB + n / (DT / VB); };
 
-  // ---- where tokens lie.  A group's tile n is 16 tokens from tile_at(n) on.
-  // Pages of whole tiles: lane l looks up tile n0 + l; else token l % 16 of tile
-  // n0 + l / 16.
+  // ---- where tokens lie.  A group's run n is 16 tokens from run_at(n) on, two of
+  // them a step.  Pages of whole runs: lane l looks up run n0 + l; else token
+  // l % 16 of run n0 + l / 16.
   constexpr int BATCH = WHOLE ? kLanes : kLanes / 16;
-  auto tile_at = [&](int n) { return p0 + (n / NT * KG + kg) * NT * 16 + n % NT * 16; };
+  auto run_at = [&](int n) { return p0 + ((n >> 1) * KG + kg) * 32 + (n & 1) * 16; };
   auto look = [&](int n0, uint32_t &page, int &slot) {
-    const int tok = WHOLE ? tile_at(n0 + lane) : tile_at(n0 + (lane >> 4)) + c16;
+    const int tok = WHOLE ? run_at(n0 + lane) : run_at(n0 + (lane >> 4)) + c16;
     const int e = over_page(kv, min(tok, max(end - 1, 0)));
     const uint32_t pg = table[min(e, last_entry)];
     slot = max(min(tok, end - 1), 0) - e * T;
@@ -301,18 +282,19 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   };
 
   // ---- loads.  A token's 16-byte pieces lie in LDS in another order for each
-  // of sixteen tokens, so that the pieces that half a wave reads at once fall on
-  // different banks (of 64): one of sixteen tokens (keys), four neighbouring ones
-  // of four or two of eight (values).
+  // of sixteen tokens, so that what is read at once falls on different banks (of
+  // 64): one piece of tokens 0-3, 12-15, 20-27 or of the others (keys; measured to
+  // be the lanes of 16-byte reads that go together), four neighbouring ones of four
+  // tokens, or two of 0-3 and 8-11 (values, 16 bits and fp8).
   auto swap_of = [](int row) {
-    return FP8 ? (row & 7) << 1 | row >> 3 : (row & 3) << 2 | row >> 2;
+    return FP8 ? (row & 3) << 1 | (row & 8) | ((row >> 2) & 1) : (row & 3) << 2 | ((row >> 2) & 3);
   };
-  auto turn_swap_of = [](int row) { return FP8 ? row >> 2 : row >> 1; };
+  auto turn_swap_of = [](int row) { return FP8 ? (row >> 2) & 3 : (row >> 1) & 7; };
   const uint32_t ring_at = uniform((uint32_t)(uintptr_t)(lds_u8 *)ring);
-  const bool full = C == CT && R == kTurn;
   constexpr int TL = RR / 16;  // lanes of a token's turned part
   // (the swap of a sum of rows whose bits differ is the swaps' together)
-  const int lat_row = lane / LPR, turn_row = (lane / TL) & 7;
+  // a load takes the turned parts of eight tokens, in fp8 of all of a run
+  const int lat_row = lane / LPR, turn_row = lane / TL;
   const uint32_t lat_piece = ((lane % LPR) ^ swap_of(lat_row)) << 4,
                  turn_piece = ((lane % TL) ^ turn_swap_of(turn_row)) << 4;
   uint32_t load_page = ~0u;
@@ -323,26 +305,25 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   struct Eight {
     const uint8_t *from;
     uint32_t to;  // the tile
-    int half, last, at_n;
-    uint32_t rows;  // all ones, or zero
-    uint32_t lanes;
+    int at, last, at_n;
+    uint32_t rows, there;  // all ones, or zero
   };
   auto eight_of = [&](int step, int e) {
-    const int eight = qg * EIGHTS + e, n = step * NT + (eight >> 1);
+    const int eight = qg + QW * e, n = step * 2 + (eight >> 1);
     if (n - load_n0 >= BATCH) {
       load_n0 = n - n % BATCH;
       look(load_n0, load_page, load_slot);
     }
     Eight x;
-    x.half = (eight & 1) * 8;
-    x.to = ring_at + (step % NST) * STAGE + (kg * NT + (eight >> 1)) * TILE;
+    x.at = eight * 8;
+    x.to = ring_at + (step % NST) * STAGE + kg * TILE;
     x.at_n = n - load_n0;
-    x.lanes = step < n_steps ? ~0u : 0;
+    x.there = step < n_steps;
     if constexpr (WHOLE) {
       const uint32_t page = __builtin_amdgcn_readlane(load_page, x.at_n);
       const uint32_t slot = __builtin_amdgcn_readlane(load_slot, x.at_n);
       x.rows = page == ~0u ? 0 : ~0u;
-      x.last = min(max(end - tile_at(n), 1), 16) - 1;
+      x.last = min(max(end - run_at(n), 1), 16) - 1;
       x.from = page == ~0u ? reinterpret_cast<const uint8_t *>(&kZeros)
                            : kv.base + ((uint64_t)page * (uint32_t)kv.piece + slot * row_bytes);
     }
@@ -352,61 +333,60 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   // past a part stay the zeros that they were.
   auto load_one = [&](const Eight &x, int i) {
     const bool turn = i == NI;
-    const uint32_t lds = turn ? x.to + 16 * RC + x.half * RR : x.to + x.half * RC + i * 1024;
-    const int at = turn ? x.half : x.half + i * RPI, row = at + (turn ? turn_row : lat_row);
+    const int at = turn ? (FP8 ? x.at & ~15 : x.at) : x.at + i * RPI;
+    const int row = (at & 15) + (turn ? turn_row : lat_row);  // of the run
+    const uint32_t lds = turn ? x.to + 32 * RC + at * RR : x.to + at * RC;
     const uint32_t piece =
         turn ? turn_piece ^ (turn_swap_of(at) << 4) : lat_piece ^ (swap_of(at) << 4);
-    // of all lanes; of half of them: eight tokens' turned parts are 512 bytes in fp8
-    uint32_t low = x.lanes, high = turn && FP8 ? 0 : x.lanes;
-    if (!full) {
-      const uint64_t there = __ballot(piece < (uint32_t)((turn ? R : C) * EB));
-      low &= (uint32_t)there;
-      high &= (uint32_t)(there >> 32);
-    }
-    const uint64_t lanes = (uint64_t)uniform(high) << 32 | uniform(low);
-    if constexpr (WHOLE) {
-      const uint32_t off = __umul24(min(row, x.last), row_bytes) + piece + (turn ? C * EB : 0);
-      to_lds(lds, x.from, off & x.rows, lanes);
+    if constexpr (MODE == kPlain) {
+      const uint32_t off = __umul24(min(row, x.last), row_bytes) + piece + (turn ? RC : 0);
+      to_lds(lds, x.from, off & x.rows, x.there);
     } else {
-      const uint32_t page = __shfl(load_page, x.at_n * 16 + row);
-      const int slot = __shfl(load_slot, x.at_n * 16 + row);
-      const uint8_t *p = kv.base + ((uint64_t)page * (uint32_t)kv.piece +
-                                    (uint32_t)slot * row_bytes + (turn ? C * EB : 0) + piece);
-      if (page == ~0u) p = reinterpret_cast<const uint8_t *>(&kZeros);
-      to_lds(lds, p, lanes);
+      const uint8_t *p;
+      if constexpr (WHOLE) {
+        p = x.from +
+            ((__umul24(min(row, x.last), row_bytes) + piece + (turn ? C * EB : 0)) & x.rows);
+      } else {
+        const uint32_t page = __shfl(load_page, x.at_n * 16 + row);
+        const int slot = __shfl(load_slot, x.at_n * 16 + row);
+        p = kv.base + ((uint64_t)page * (uint32_t)kv.piece + (uint32_t)slot * row_bytes +
+                       (turn ? C * EB : 0) + piece);
+        if (page == ~0u) p = reinterpret_cast<const uint8_t *>(&kZeros);
+      }
+      const uint64_t in = __ballot(piece < (uint32_t)((turn ? R : C) * EB));
+      to_lds_some(lds, p, x.there,
+                  (uint64_t)uniform((uint32_t)(in >> 32)) << 32 | uniform((uint32_t)in));
     }
   };
 
   float m = kNegInf, l = 0.f;
-  f32x16 o[DT - VT], ov[VT + 1];
+  f32x16 o[DT];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT - VT; ++dt) o[dt][i] = 0.f;
-    if (VT) ov[0][i] = 0.f;
-  }
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   uint32_t odd = 0;
 
   // Places of this lane's reads in a tile: of keys, of turned parts, of values.
   // Which pieces of sixteen are read turns bits 4 to 7 of the place, which are the
   // low bits of a piece; tiles and rows are whole 256 bytes (turned parts 64, 128).
-  const uint32_t key_at = c16 * RC + ((g ^ swap_of(c16)) << 4);
-  const uint32_t turn_at =
-      16 * RC + c16 * RR + (((g & (TL - 1)) ^ turn_swap_of(c16)) << 4);
-  const int val_row = h * 8 + (FP8 ? c16 >> 1 : c16 >> 2);
+  const uint32_t key_at = c * RC + ((h ^ swap_of(c)) << 4);
+  const uint32_t turn_at = 32 * RC + c * RR + ((h ^ turn_swap_of(c)) << 4);
+  // of values the first sixteen tokens': those that a lane's scores are of
+  const int val_row = FP8 ? (c16 >> 3) * 8 + h * 4 + ((c16 >> 1) & 3) : h * 4 + (c16 >> 2);
   const uint32_t val_at =
       val_row * RC + (c16 & 1) * 8 +
       (((FP8 ? g & 1 : (g & 1) * 2 + ((c16 >> 1) & 1)) ^ swap_of(val_row)) << 4);
 
-  // Of the batch of tiles that is computed: which pages are not there; the scales
-  // of latents, and times scale_log2 of the scores' two parts; the former's
-  // logarithm, within bounds.
+  // Of the batch of runs that is computed: which pages are not there; the scales
+  // of latents, times scale_log2, its logarithm (within bounds); of turned parts in
+  // units of the former, which is held to 2^-60 of them for that.
   uint64_t gone_of = 0;
-  float sc_of = 1.f, sc2_of = 1.f, sr2_of = 1.f, log_of = 0.f;
+  float sc_of = 1.f, sc2_of = 1.f, sr_of = 1.f, log_of = 0.f;
   int n0_of = -(1 << 20);
   auto batch = [&](int step) {
-    if (step * NT - n0_of < BATCH) return;
-    n0_of = step * NT - step * NT % BATCH;
+    if (step * 2 - n0_of < BATCH) return;
+    n0_of = step * 2 - step * 2 % BATCH;
     uint32_t page;
     int slot;
     look(n0_of, page, slot);
@@ -416,38 +396,41 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
       float sc = sp[0], sr = sp[1];
       here(sc);
       here(sr);
-      sc_of = page == ~0u ? 1.f : sc;
-      sc2_of = sc_of * a.scale_log2;
-      sr2_of = (page == ~0u ? 1.f : sr) * a.scale_log2;
-      log_of = __log2f(fmaxf(fabsf(sc_of), 0x1p-60f));
+      if (page == ~0u) sc = sr = 1.f;
+      const float least = fmaxf(fabsf(sr) * 0x1p-60f, 0x1p-100f);
+      sc_of = sc;
+      if (fabsf(sc) < least) sc = sc < 0.f ? -least : least;
+      sc2_of = sc * a.scale_log2;
+      sr_of = sr / sc;
+      log_of = __log2f(fmaxf(fabsf(sc), 0x1p-60f));
     }
   };
 
-  // The i-th piece of a token's key that is read, and of Q beside it: those whose
-  // places differ by whole 256 bytes one after another.
-  constexpr int KQ = KC / 4;
-  auto key_of = [](int i) { return i < KC ? i % KQ * 4 + i / KQ : i; };
+  // The i-th piece of a token's key that is read: the turned part's, then those
+  // whose places differ by whole 256 bytes one after another; and of Q beside it.
+  constexpr int KB = 8, KQ = KC / KB;  // reads of two halves of 16 pieces
+  auto key_of = [](int i) { return i < KR ? KC + i : (i - KR) % KQ * KB + (i - KR) / KQ; };
   auto key_piece = [&](uint32_t tile, int i) {
     const int k = key_of(i);
-    const uint32_t at = k >= KC ? (tile + turn_at) ^ ((k - KC) << 6)
-                                : ((tile + key_at) ^ ((k & 3) << 6)) + (k >> 2) * 256;
+    const uint32_t at = k >= KC ? (tile + turn_at) ^ ((k - KC) << 5)
+                                : ((tile + key_at) ^ ((k & 7) << 5)) + (k >> 3) * 256;
     return *reinterpret_cast<lds_u32x4 *>(at);
   };
-  // A tile's values: eight tokens of an element for each of 32.
+  // Values of sixteen tokens: a lane's eight of them for each of 32 elements.
   struct Values {
     u32x2 w[FP8 ? 1 : 2];
   };
-  auto value_piece = [&](uint32_t tile, int dt) {
+  auto value_piece = [&](uint32_t run, int dt) {
     Values v;
     if constexpr (FP8) {
-      const uint32_t at = ((tile + val_at) ^ ((dt & 7) << 5)) + (dt >> 3) * 256;
+      const uint32_t at = ((run + val_at) ^ ((dt & 7) << 5)) + (dt >> 3) * 256;
       v.w[0] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                                              reinterpret_cast<lds_i32x2 *>(at)));
     } else {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t at =
-            ((tile + val_at) ^ ((dt & 3) << 6 | j << 4)) + (dt >> 2) * 256 + j * 4 * RC;
+      for (int j = 0; j < 2; ++j) {  // eight tokens on
+        const uint32_t at = ((run + val_at) ^ ((dt & 3) << 6 | (swap_of(8) << 4) * j)) +
+                            (dt >> 2) * 256 + j * 8 * RC;
         v.w[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                                reinterpret_cast<lds_s16x4 *>(at)));
       }
@@ -457,12 +440,11 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
 
   // Zeros in place of a tile's values that are not finite, once every wave that
   // shares it has read its keys.
-  auto mend = [&](int step, int kt) {
+  auto mend = [&](int step) {
     if (QW > 1) __syncthreads();
-    uint8_t *p = ring + (step % NST) * STAGE + (kg * NT + kt) * TILE + qg * (16 / QW) * RC +
-                 lane * 16;
+    uint8_t *p = ring + (step % NST) * STAGE + kg * TILE + qg * (32 / QW) * RC + lane * 16;
 #pragma unroll 1
-    for (int i = 0; i < 16 / QW * RC / 1024; ++i) {
+    for (int i = 0; i < 32 / QW * RC / 1024; ++i) {
       u32x4 v = *reinterpret_cast<u32x4 *>(p + i * 1024);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -476,92 +458,73 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
     else wait_reads();
   };
 
-  // ---- a tile's scores, S^T = K Q^T: columns c16 of two sixteens, tokens
-  // g * 4 + i; beside each read's products something else, side(k)
-  f32x4 x[2], xr[2];
-  auto scores = [&](uint32_t tile, auto before, auto side) {
+  // ---- a tile's scores, S^T = K Q^T: column c, tokens (i / 4) * 8 + h * 4 +
+  // i % 4; beside each read's products something else, side(i).  fp8: the turned
+  // part's come first and go into units of the latents' scale.
+  f32x16 x;
+  auto scores = [&](int step, auto side) {
+    const uint32_t tile = ring_at + (step % NST) * STAGE + kg * TILE;
     u32x4 w[AHEAD + 1];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) w[k] = key_piece(tile, k);
+    for (int i = 0; i < AHEAD; ++i) w[i] = key_piece(tile, i);
     __builtin_amdgcn_sched_barrier(0);
-    before();
 #pragma unroll
-    for (int nb = 0; nb < 2; ++nb) {
-      x[nb] = {0.f, 0.f, 0.f, 0.f};
-      if (FP8) xr[nb] = {0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int k = 0; k < KC + KR; ++k) {
-      if (k + AHEAD < KC + KR) w[(k + AHEAD) % (AHEAD + 1)] = key_piece(tile, k + AHEAD);
+    for (int i = 0; i < KN; ++i) {
+      if (i + AHEAD < KN) w[(i + AHEAD) % (AHEAD + 1)] = key_piece(tile, i + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
-      const u32x4 v = w[k % (AHEAD + 1)];
+      const u32x4 v = w[i % (AHEAD + 1)];
       if constexpr (FP8) {
-        f32x4 *to = k >= KC ? xr : x;
+        const u32x4 lo = {fp8_pair<ACT, false>(v[0]), fp8_pair<ACT, true>(v[0]),
+                          fp8_pair<ACT, false>(v[1]), fp8_pair<ACT, true>(v[1])};
+        const u32x4 hi = {fp8_pair<ACT, false>(v[2]), fp8_pair<ACT, true>(v[2]),
+                          fp8_pair<ACT, false>(v[3]), fp8_pair<ACT, true>(v[3])};
+        if (i == 0) multiply32<ACT, true, true>(x, lo, qreg[2 * key_of(i)]);
+        else multiply32<ACT, false, true>(x, lo, qreg[2 * key_of(i)]);
+        multiply32<ACT, false, true>(x, hi, qreg[2 * key_of(i) + 1]);
+        if (i == KR - 1) {
+          settled(x);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const u32x4 af = {fp8_pair<ACT, false>(v[2 * j]), fp8_pair<ACT, true>(v[2 * j]),
-                            fp8_pair<ACT, false>(v[2 * j + 1]),
-                            fp8_pair<ACT, true>(v[2 * j + 1])};
-          multiply<ACT>(to[0], to[1], af, qreg[0][2 * key_of(k) + j], qreg[1][2 * key_of(k) + j]);
+          for (int j = 0; j < 16; ++j) {
+            const int n = step * 2 + (j >> 3) - n0_of;
+            x[j] *= WHOLE ? of_lane(sr_of, n)
+                          : __shfl(sr_of, n * 16 + (j >> 2 & 1) * 8 + h * 4 + (j & 3));
+          }
         }
       } else {
-        multiply<ACT>(x[0], x[1], v, qreg[0][key_of(k)], qreg[1][key_of(k)]);
+        if (i == 0) multiply32<ACT, true, true>(x, v, qreg[key_of(i)]);
+        else multiply32<ACT, false, false>(x, v, qreg[key_of(i)]);
       }
-      side(k);
+      side(i);
       __builtin_amdgcn_sched_barrier(0);
     }
+    settled(x);
   };
 
-  // ---- its weights: scores exchanged so that a lane has tokens h * 8 + 0 .. 7 of
-  // column c, as the second product takes them, masked
-  float y[8], vs[FP8 ? 8 : 1], ls = 0.f;
-  auto exchange = [&](int n) {
-    settled(x[0], x[1]);
-    if (FP8) settled(xr[0], xr[1]);
-    const int at_n = n - n0_of, tok0 = tile_at(n);
-    float sc[4], sr[4];
-    if constexpr (FP8 && WHOLE) {
-      sc[0] = of_lane(sc2_of, at_n);
-      sr[0] = of_lane(sr2_of, at_n);
-      vs[0] = of_lane(sc_of, at_n);
-      ls = of_lane(log_of, at_n);
+  // ---- its weights, masked
+  float y[16], vs[FP8 ? 16 : 1];
+  float ls[2] = {0.f, 0.f};
+  auto mask = [&](int step) {
 #pragma unroll
-      for (int i = 1; i < 8; ++i) vs[i] = vs[0];
+    for (int i = 0; i < 16; ++i) y[i] = x[i];
+    const int n = step * 2 - n0_of, tok0 = run_at(step * 2);
+    if constexpr (FP8) {
 #pragma unroll
-      for (int i = 1; i < 4; ++i) {
-        sc[i] = sc[0];
-        sr[i] = sr[0];
-      }
-    } else if constexpr (FP8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[i] = __shfl(sc2_of, at_n * 16 + g * 4 + i);
-        sr[i] = __shfl(sr2_of, at_n * 16 + g * 4 + i);
+      for (int i = 0; i < 16; ++i) {
+        const int r = n + (i >> 3), at = r * 16 + (i >> 2 & 1) * 8 + h * 4 + (i & 3);
+        y[i] *= WHOLE ? of_lane(sc2_of, r) : __shfl(sc2_of, at);
+        vs[i] = WHOLE ? of_lane(sc_of, r) : __shfl(sc_of, at);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vs[i] = __shfl(sc_of, at_n * 16 + h * 8 + i);
+      for (int r = 0; r < 2; ++r) ls[r] = WHOLE ? of_lane(log_of, n + r) : 0.f;
     }
+    const uint32_t gone = WHOLE ? ((gone_of >> n) & 1 ? 0xffffu : 0u) |
+                                      ((gone_of >> (n + 1)) & 1 ? 0xffff0000u : 0u)
+                                : (uint32_t)(gone_of >> (n * 16));
+    if (gone || tok0 + 32 > all_lim) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float u = x[0][i], v = x[1][i];
-      if constexpr (FP8) {
-        u = u * sc[i] + xr[0][i] * sr[i];
-        v = v * sc[i] + xr[1][i] * sr[i];
-      } else {
-        u *= a.scale_log2;
-        v *= a.scale_log2;
-      }
-      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v),
-                                                      false, false);
-      y[i] = __uint_as_float(r[0]);
-      y[4 + i] = __uint_as_float(r[1]);
-    }
-    const uint32_t gone = WHOLE ? ((gone_of >> at_n) & 1 ? 0xffffu : 0u)
-                                : (uint32_t)(gone_of >> (at_n * 16)) & 0xffffu;
-    if (gone || tok0 + 16 > all_lim) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool out = tok0 + h * 8 + i >= lim || ((gone >> (h * 8 + i)) & 1);
+      for (int i = 0; i < 16; ++i) {
+        const int at = (i >> 2) * 8 + h * 4 + (i & 3);
+        const bool out = tok0 + at >= lim || ((gone >> at) & 1);
         y[i] = out ? kNegInf : y[i];
         // (a scale that is not finite, or one of a block that the row sees
         // nothing of)
@@ -572,63 +535,58 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   // The weights in kSides pieces of about the same work, to stand between
   // products.  The reference counts a value's scale in, within bounds, so that its
   // weight with the scale fits 16 bits.
-  constexpr int kSides = 16;
+  constexpr int kSides = 28;
+  const float of_score = FP8 ? 1.f : a.scale_log2;
   float top, f, ref;
   uint64_t jump = 0;
-  u32x4 ph, pl;
+  u32x4 ph[2], pl[2];
   auto weigh = [&](int i) {
-    if (i == 0) {
-      if constexpr (FP8 && !WHOLE) {
-        top = kNegInf;
+    if (i == 0 || i == 1) {
+      float t = kNegInf;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          top = fmaxf(top, y[j] + __log2f(fmaxf(fabsf(vs[j]), 0x1p-60f)));
-      } else {
-        top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])),
-                    fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+      for (int j = i * 8; j < i * 8 + 8; ++j) {
+        if constexpr (FP8 && !WHOLE) t = fmaxf(t, y[j] + __log2f(fmaxf(fabsf(vs[j]), 0x1p-60f)));
+        else t = fmaxf(t, y[j]);
       }
-    } else if (i == 1) {
-      if constexpr (FP8 && WHOLE) top += ls;
-      top = max_rows32(top);
+      if constexpr (FP8 && WHOLE) t += ls[i];
+      top = i == 0 ? t : fmaxf(top, t);
     } else if (i == 2) {
+      top = max_rows32(top) * of_score;
+    } else if (i == 3) {
       const bool over = top > m + kSlack;
       jump = __ballot(over);
       top = over ? top : m;
       f = m == kNegInf ? 0.f : exp2_fast(m - top);
-    } else if (i == 3) {
       l *= f;
       m = top;
       ref = m == kNegInf ? 0.f : m - kShift;
-    } else if (i < 12) {
-      float &p = y[i - 4];
-      p = exp2_fast(p - ref);
-      l += p;
-      if constexpr (FP8) p *= vs[i - 4];
     } else {
-      const int w = i - 12;
-      const uint32_t hi = pack_act<PV>(y[2 * w], y[2 * w + 1]);
-      ph[w] = hi;
-      if constexpr (HILO)
-        pl[w] = pack_act<kBf16>(y[2 * w] - __uint_as_float(hi << 16),
-                                y[2 * w + 1] - __uint_as_float(hi & 0xffff0000u));
-    }
-  };
-  // ---- O^T += V^T P^T, loads of later tokens between the products
-  Values vw[VAHEAD + 1];
-  auto add_values = [&](uint32_t tile, auto side) {
-    if (jump) {
-      rescale(o, f);
-      if (VT) {
-        settled(ov[0]);
-        ov[0] *= f;
+      const int j = (i - 4) / 3, part = (i - 4) % 3;  // pair j of values
+      if (part < 2) {
+        float &p = y[2 * j + part];
+        p = exp2_fast(p * of_score - ref);
+        l += p;
+        if constexpr (FP8) p *= vs[2 * j + part];
+      } else {
+        const uint32_t hi = pack_act<PV>(y[2 * j], y[2 * j + 1]);
+        ph[j >> 2][j & 3] = hi;
+        if constexpr (HILO)
+          pl[j >> 2][j & 3] = pack_act<kBf16>(y[2 * j] - __uint_as_float(hi << 16),
+                                              y[2 * j + 1] - __uint_as_float(hi & 0xffff0000u));
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  // ---- O^T += V^T P^T of sixteen tokens, loads of later ones between the products
+  Values vw[VAHEAD + 1];
+  auto values_ahead = [&](uint32_t run) {
+#pragma unroll
+    for (int n = 0; n < VAHEAD; ++n) vw[n] = value_piece(run, tile_of_sum(n));
+  };
+  auto add_values = [&](uint32_t run, int half, auto side) {
 #pragma unroll
     for (int n = 0; n < DT; ++n) {
-      const int dt = tile_of_sum(n);
       if (n + VAHEAD < DT)
-        vw[(n + VAHEAD) % (VAHEAD + 1)] = value_piece(tile, tile_of_sum(n + VAHEAD));
+        vw[(n + VAHEAD) % (VAHEAD + 1)] = value_piece(run, tile_of_sum(n + VAHEAD));
       __builtin_amdgcn_sched_barrier(0);
       const Values v = vw[n % (VAHEAD + 1)];
       u32x4 af;
@@ -637,34 +595,31 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
                    fp8_pair<PV, false>(v.w[0][1]), fp8_pair<PV, true>(v.w[0][1])};
       else
         af = u32x4{v.w[0][0], v.w[0][1], v.w[1][0], v.w[1][1]};
-      if (dt < DT - VT) {
-        f32x16 &to = o[dt < DT - VT ? dt : 0];
-        to = mfma32<PV>(af, ph, to);
-        if constexpr (HILO) to = mfma32<PV>(af, pl, to);
-      } else {
-        multiply32<PV>(ov[0], af, ph);
-        if constexpr (HILO) multiply32<PV>(ov[0], af, pl);
-      }
+      f32x16 &to = o[tile_of_sum(n)];
+      to = mfma32<PV>(af, ph[half], to);
+      if constexpr (HILO) to = mfma32<PV>(af, pl[half], to);
       side(n);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  // ---- the ring: loads are NST - 1 steps ahead, issued between products.  The
-  // scores of a tile are made beside the weights of the one before it, where there
-  // is room for three steps.  Steps past the last
-  // load nothing, and what is made of their tokens goes unused.
-  if (!full) {  // pieces past a token's parts
+  // ---- the ring.  With room for three steps or more, a tile's scores are made
+  // beside the weights of the one before it, and loads go on all the time, NST - 1
+  // steps ahead.  With room for two, sixteen tokens' place is loaded into once their
+  // values have been used.  Loads stand between products: the way to LDS takes 64
+  // bytes a cycle of all waves, and one that waits for it holds up its wave.  Steps
+  // past the last load nothing, and what is made of their tokens goes unused.
+  if (MODE != kPlain) {  // pieces past a token's parts
     for (int i = threadIdx.x * 16; i < NST * STAGE; i += kThreads * 16)
       *reinterpret_cast<u32x4 *>(ring + i) = u32x4{0, 0, 0, 0};
     __syncthreads();
   }
-  auto tile_of = [&](int step, int kt) {
-    return ring_at + (step % NST) * STAGE + (kg * NT + kt) * TILE;
+  auto meet = [&] {  // all waves have read what they wanted of the ring
+    wait_reads();
+    if (QW > 1) __syncthreads();
   };
-  auto nothing = [](int) {};
-  constexpr int FIRST = PIPE ? NST - 1 : NST;  // steps that load before the first
   if (n_steps > 0) {
+    constexpr int FIRST = PIPE ? NST - 1 : 2;  // steps that load before the first
     batch(0);
 #pragma unroll 1
     for (int step = 0; step < FIRST; ++step)
@@ -674,79 +629,68 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
 #pragma unroll
         for (int i = 0; i <= NI; ++i) load_one(from, i);
       }
-    wait_loads<(FIRST - 1) * LOADS>();
+    if (FIRST <= n_steps) wait_loads<(FIRST - 1) * LOADS>();
+    else wait_loads<0>();
     if (QW > 1) __syncthreads();
-    scores(tile_of(0, 0), [] {}, nothing);
+    scores(0, [](int) {});
 #pragma unroll 1
     for (int step = 0; step < n_steps; ++step) {
-      batch(step);
-      // some row attends to a token here that another does not
+      const uint32_t tile = ring_at + (step % NST) * STAGE + kg * TILE;
+      // where rows attend to different tokens, values that are not finite count as
+      // zero and are left for the end
       const int first = p0 + step * STEP;
-      const bool cut = all_lim < end && first + STEP > all_lim;
+      if (all_lim < end && first + STEP > all_lim) mend(step);
+      mask(step);
+      batch(step + 1);
       Eight from[EIGHTS];
-      auto load_next = [&](int i) {  // of the step's loads
-        if (i < LOADS) load_one(from[i / (NI + 1)], i % (NI + 1));
+      // loads in even distances over `of` places
+      auto load_at = [&](int at, int of, int i0, int count) {
+#pragma unroll
+        for (int i = 0; i < count; ++i)
+          if ((2 * i + 1) * of / (2 * count) == at)
+            load_one(from[(i0 + i) / (NI + 1)], (i0 + i) % (NI + 1));
       };
+      constexpr int EACH = (kSides + KN - 1) / KN;
+      if constexpr (PIPE) {
+        // (no more loads than these are on their way while there are steps to load)
+        if (step + NST - 2 < n_steps) wait_loads<(PIPE ? NST - 3 : 0) * LOADS>();
+        else wait_loads<0>();
+        meet();
 #pragma unroll
-      for (int kt = 0; kt < NT; ++kt) {
-        const uint32_t tile = tile_of(step, kt);
-        const bool last = kt == NT - 1;
-        // Where rows attend to different tokens, values that are not finite count
-        // as zero and are left for the end
-        if (cut) mend(step, kt);
-        constexpr int EACH = (kSides + KC + KR - 1) / (KC + KR);
-        constexpr int LEACH = (LOADS + DT - 1) / DT, KEACH = (LOADS + KC + KR - 1) / (KC + KR);
-        auto value_ahead = [&](int k) {
-          const int n = k - (KC + KR - VAHEAD);
-          if (n >= 0) vw[n] = value_piece(tile, tile_of_sum(n));
-        };
-        if constexpr (PIPE) {
-          if (last) {
-            wait_loads<(NST - 3) * LOADS>();
-            wait_reads();
-            if (QW > 1) __syncthreads();
+        for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + NST - 1, e);
+        scores(step + 1, [&](int k) {
 #pragma unroll
-            for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + NST - 1, e);
-          }
-          scores(last ? tile_of(step + 1, 0) : tile_of(step, kt + 1),
-                 [&] { exchange(step * NT + kt); },
-                 [&](int k) {
+          for (int i = 0; i < EACH; ++i)
+            if (k * EACH + i < kSides) weigh(k * EACH + i);
+          load_at(k, KN, 0, LOADS / 2);
+          if (k == KN - 2) values_ahead(tile);
+        });
+        if (jump) rescale(o, f);
+        add_values(tile, 0, [&](int n) { load_at(n, 2 * DT, LOADS / 2, LOADS - LOADS / 2); });
+        values_ahead(tile + 16 * RC);
+        add_values(tile + 16 * RC, 1,
+                   [&](int n) { load_at(DT + n, 2 * DT, LOADS / 2, LOADS - LOADS / 2); });
+      } else {
+        constexpr int HALF = LOADS / 2;
+        values_ahead(tile);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                   for (int i = 0; i < EACH; ++i)
-                     if (k * EACH + i < kSides) weigh(k * EACH + i);
-                   value_ahead(k);
-                 });
-          add_values(tile, [&](int n) {
+        for (int i = 0; i < kSides; ++i) weigh(i);
+        if (jump) rescale(o, f);
+        add_values(tile, 0, [](int) {});
+        values_ahead(tile + 16 * RC);
+        meet();
 #pragma unroll
-            for (int i = 0; i < LEACH; ++i)
-              if (last) load_next(n * LEACH + i);
-          });
-        } else {
-          exchange(step);
-#pragma unroll
-          for (int n = 0; n < VAHEAD; ++n) vw[n] = value_piece(tile, tile_of_sum(n));
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int i = 0; i < kSides; ++i) weigh(i);
-          add_values(tile, nothing);
-          wait_loads<0>();
-          wait_reads();
-          if (QW > 1) __syncthreads();
-#pragma unroll
-          for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + NST, e);
-          scores(tile_of(step + 1, 0), [] {},
-                 [&](int k) {
-#pragma unroll
-                   for (int i = 0; i < KEACH; ++i) load_next(k * KEACH + i);
-                 });
-        }
+        for (int e = 0; e < EIGHTS; ++e) from[e] = eight_of(step + 2, e);
+        add_values(tile + 16 * RC, 1, [&](int n) { load_at(n, DT, 0, HALF); });
+        if (step + 2 < n_steps) wait_loads<HALF>();
+        else wait_loads<0>();
+        meet();
+        scores(step + 1, [&](int k) { load_at(k, KN, HALF, HALF); });
       }
     }
     wait_loads<0>();
   }
-  if (VT) settled(ov[0]);
-  auto sum_at = [&](int dt, int i) { return dt < DT - VT ? o[dt < DT - VT ? dt : 0][i] : ov[0][i]; };
-
   // ---- values that are not finite, where not every row attends to them: a
   // weight that is not zero made the whole row NaN, zero times them is NaN too
   if (!FP8 && __syncthreads_or(odd != 0)) {
@@ -758,7 +702,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
       if (page >= (uint32_t)kv.num_pages) continue;
       const uint16_t *p = reinterpret_cast<const uint16_t *>(
           kv.base + ((uint64_t)page * (uint32_t)kv.piece + (uint32_t)(at - e * T) * row_bytes));
-      const bool sees = at < lim && (at - p0) / (NT * 16) % KG == kg;
+      const bool sees = at < lim && (at - p0) / 32 % KG == kg;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -772,12 +716,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
             add[i] = d < C && sees && (bad[i >> 1] >> (16 * (i & 1)) & 0xffff)
                          ? __uint_as_float(0x7fc00000u)
                          : 0.f;
-          if (dt < DT - VT) {
-            add4(o[dt < DT - VT ? dt : 0], i4, add);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ov[0][i4 * 4 + i] += add[i];
-          }
+          add4(o[dt], i4, add);
         }
         __builtin_amdgcn_sched_barrier(0);  // a block's loads at a time: registers
       }
@@ -821,8 +760,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4)
         emit(dt, i4,
-             f32x4{sum_at(dt, i4 * 4), sum_at(dt, i4 * 4 + 1), sum_at(dt, i4 * 4 + 2),
-                   sum_at(dt, i4 * 4 + 3)},
+             f32x4{o[dt][i4 * 4], o[dt][i4 * 4 + 1], o[dt][i4 * 4 + 2],
+                   o[dt][i4 * 4 + 3]},
              norm);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -853,8 +792,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
         for (int i4 = 0; i4 < 4; ++i4) {
           const int dt = round * RD + d;
           sums[((wave * RD + d) * 4 + i4) * kLanes + lane] =
-              f32x4{sum_at(dt, i4 * 4) * f, sum_at(dt, i4 * 4 + 1) * f,
-                    sum_at(dt, i4 * 4 + 2) * f, sum_at(dt, i4 * 4 + 3) * f};
+              f32x4{o[dt][i4 * 4] * f, o[dt][i4 * 4 + 1] * f,
+                    o[dt][i4 * 4 + 2] * f, o[dt][i4 * 4 + 3] * f};
         }
       __syncthreads();
       for (int d = kg; d < RD; d += KG)
@@ -938,12 +877,15 @@ void go(void (*kernel)(LatentAttendArgs), const LatentAttendArgs &a, hipStream_t
   hipLaunchKernelGGL(kernel, dim3((unsigned)a.split_grid), dim3(kThreads), 0, s, a);
 }
 
-template <int ACT, bool FP8, int CT, bool WHOLE>
+template <int ACT, bool FP8, int CT, Mode MODE>
 hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
   switch (a.wave_columns) {
-    case 1: go(attend_latent<ACT, FP8, CT, 1, WHOLE>, a, s); break;
-    case 2: go(attend_latent<ACT, FP8, CT, 2, WHOLE>, a, s); break;
-    default: go(attend_latent<ACT, FP8, CT, 4, WHOLE>, a, s);
+    case 1:  // (two steps of 16-bit tokens would not fit)
+      if constexpr (FP8) go(attend_latent<ACT, FP8, CT, 1, MODE>, a, s);
+      else return hipErrorInvalidValue;
+      break;
+    case 2: go(attend_latent<ACT, FP8, CT, 2, MODE>, a, s); break;
+    default: go(attend_latent<ACT, FP8, CT, 4, MODE>, a, s);
   }
   if (a.slices > 0)
     hipLaunchKernelGGL(join_latent<ACT>,
@@ -952,13 +894,16 @@ hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int ACT, bool FP8, int CT>
+hipError_t rows(const LatentAttendArgs &a, hipStream_t s) {
+  if (a.kv.page_tokens % 16 != 0) return columns<ACT, FP8, CT, kPages>(a, s);
+  if (a.latent != CT || a.turn != kTurn) return columns<ACT, FP8, CT, kRows>(a, s);
+  return columns<ACT, FP8, CT, kPlain>(a, s);
+}
+
 template <int ACT, bool FP8>
 hipError_t latents(const LatentAttendArgs &a, hipStream_t s) {
-  if (a.kv.page_tokens % 16 == 0)
-    return a.latent <= 256 ? columns<ACT, FP8, 256, true>(a, s)
-                           : columns<ACT, FP8, 512, true>(a, s);
-  return a.latent <= 256 ? columns<ACT, FP8, 256, false>(a, s)
-                         : columns<ACT, FP8, 512, false>(a, s);
+  return a.latent <= 256 ? rows<ACT, FP8, 256>(a, s) : rows<ACT, FP8, 512>(a, s);
 }
 
 }  // namespace

@@ -176,7 +176,7 @@ constexpr int32_t split_resident(int32_t head_dim, int32_t columns) {
 }
 
 // Tokens of a step of the latent kernel with this many groups of 32 columns.
-constexpr int32_t latent_step(int32_t wave_columns) { return wave_columns == 1 ? 64 : 32; }
+constexpr int32_t latent_step(int32_t wave_columns) { return 128 / wave_columns; }
 
 // Counters at the start of an attention workspace: a unit's parts done.  More
 // units than kSplitUnits are not split.

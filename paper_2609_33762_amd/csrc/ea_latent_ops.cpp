@@ -28,7 +28,8 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *
   Parts p{};
   const int64_t most = (int64_t)b->max_rows * a->q_heads;
   const int cus = compute_units(ea::cache_device(c));
-  p.wave_columns = most <= 32 ? 1 : most <= 64 ? 2 : 4;
+  const int least = ea::cache_desc(c).elem_bytes == 1 ? 1 : 2;
+  p.wave_columns = most <= 32 ? least : most <= 64 ? 2 : 4;
   p.wave_columns = env("EA_QW", p.wave_columns);
   const int64_t tile = 32 * p.wave_columns;
   p.tiles = (int32_t)((most + tile - 1) / tile);
