@@ -813,13 +813,18 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
 // Joins the parts of a unit's 32 rows, some tiles of 32 elements:
 //   o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i,  m = max_i m_i.
 // A launch of its own, so that many workgroups read the parts and nothing waits
-// or counts.  Wave (g, i4): a quarter of a tile's elements, every kGroups-th part.
+// or counts.  First all parts' factors, 32 rows at a time; then wave (g, i4) adds
+// a quarter of a tile's elements of every kGroups-th part.
 constexpr int kGroups = 4, kJoinThreads = kGroups * 4 * kLanes;
+constexpr int kFactors = 512;  // parts whose factors fit
 template <int ACT>
 __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) {
+  constexpr int TOGETHER = kJoinThreads / 32;
+  __shared__ float factor[kFactors][32];
+  __shared__ float each[2][TOGETHER][32];
   __shared__ f32x4 sums[kGroups][4][kLanes];
-  const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
-  const int wave = uniform((int)threadIdx.x >> 6), i4 = wave & 3, g = wave >> 2;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int wave = uniform(tid >> 6), i4 = wave & 3, g = wave >> 2;
   const int QW = a.wave_columns, HQ = a.q_heads, C = a.latent, cols = (C + 31) & ~31;
   uint32_t u = blockIdx.x;
   const int slice = u % a.slices;
@@ -831,43 +836,69 @@ __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) 
   const int r = tile * QW * 32 + qg * 32 + c, rows_all = sq.rows * HQ;
   if (r - c >= rows_all) return;
   const int w0 = a.units[2 * ((int64_t)s * a.tiles_most + tile)];
-  const int parts = a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1];
+  const int parts = min(a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1], kFactors);
   if (parts <= 1) return;
   const bool mine = r < rows_all;
   const int64_t pitch = (int64_t)(QW * 32) * (cols + 2);
   const float *first = a.parts + (int64_t)w0 * pitch;
-  const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);
-  float ref = kNegInf, total = 0.f;
-  if (mine) {
-    for (int k = 0; k < parts; ++k) ref = fmaxf(ref, ml[k * pitch]);
+  {
+    const int k0 = tid >> 5;
+    const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);
+    f32x2 v[kFactors / TOGETHER];
+    float ref = kNegInf, total = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFactors / TOGETHER; ++i) {
+      v[i] = f32x2{kNegInf, 0.f};
+      if (mine && k0 + i * TOGETHER < parts)
+        v[i] = *reinterpret_cast<const f32x2 *>(ml + (k0 + i * TOGETHER) * pitch);
+    }
+#pragma unroll
+    for (int i = 0; i < kFactors / TOGETHER; ++i) ref = fmaxf(ref, v[i][0]);
+    each[0][k0][c] = ref;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TOGETHER; ++i) ref = fmaxf(ref, each[0][i][c]);
+    const float zero = ref == kNegInf ? 0.f : ref;
+#pragma unroll
+    for (int i = 0; i < kFactors / TOGETHER; ++i) {
+      if (k0 + i * TOGETHER >= parts) break;
+      const float f = exp2_fast(v[i][0] - zero);
+      total += f * v[i][1];
+      factor[k0 + i * TOGETHER][c] = f;
+    }
+    each[1][k0][c] = total;
+    __syncthreads();
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < TOGETHER; ++i) total += each[1][i][c];
+    if (mine && slice == 0 && wave == 0 && h == 0 && a.lse)
+      a.lse[(int64_t)(sq.row0 + r / HQ) * HQ + r % HQ] =
+          total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+    const float norm = total == 0.f ? 0.f : 1.f / total;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFactors / TOGETHER; ++i)
+      if (k0 + i * TOGETHER < parts) factor[k0 + i * TOGETHER][c] *= norm;
+    __syncthreads();
   }
-  const float zero = ref == kNegInf ? 0.f : ref;
-  if (mine) {
-    for (int k = 0; k < parts; ++k) total += exp2_fast(ml[k * pitch] - zero) * ml[k * pitch + 1];
-  }
-  const float norm = total == 0.f ? 0.f : 1.f / total;
-  const int64_t row = sq.row0 + r / HQ, head = r % HQ;
-  if (mine && slice == 0 && wave == 0 && h == 0 && a.lse)
-    a.lse[row * HQ + head] =
-        total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
+  uint16_t *out = a.out.data + (int64_t)(sq.row0 + r / HQ) * a.out.row_stride +
+                  (int64_t)(r % HQ) * a.out.head_stride;
   for (int dt = slice; dt < cols / 32; dt += a.slices) {
     const int d = dt * 32 + i4 * 8 + h * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (mine && d < C) {
       const float *p = first + qg * 32 * cols + ((dt * 4 + i4) * kLanes + lane) * 4;
-#pragma unroll 4
+#pragma unroll 8
       for (int k = g; k < parts; k += kGroups)
-        acc += exp2_fast(ml[k * pitch] - zero) * *reinterpret_cast<const f32x4 *>(p + k * pitch);
+        acc += factor[k][c] * *reinterpret_cast<const f32x4 *>(p + k * pitch);
     }
     sums[g][i4][lane] = acc;
     __syncthreads();
     if (g == 0 && mine && d < C) {
 #pragma unroll
       for (int k = 1; k < kGroups; ++k) acc += sums[k][i4][lane];
-      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride +
-                                 d) =
-          u32x2{pack_act<ACT>(acc[0] * norm, acc[1] * norm),
-                pack_act<ACT>(acc[2] * norm, acc[3] * norm)};
+      *reinterpret_cast<u32x2 *>(out + d) =
+          u32x2{pack_act<ACT>(acc[0], acc[1]), pack_act<ACT>(acc[2], acc[3])};
     }
     __syncthreads();
   }

@@ -43,7 +43,7 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *
   p.grid = (int32_t)std::min<int64_t>(p.wgs + units, units * whole);
   if (p.grid > units) {
     const int64_t groups = (int64_t)b->n_seqs * p.tiles * p.wave_columns;
-    p.slices = (int32_t)std::min<int64_t>(16, std::max<int64_t>(1, 1024 / groups));
+    p.slices = (int32_t)std::min<int64_t>(16, std::max<int64_t>(1, env("EA_SL",256) / groups));
     p.unit_bytes = up((int64_t)b->n_seqs * p.tiles * 8, 16);
     p.bytes = p.unit_bytes + (int64_t)p.grid * tile * (up(a->latent_dim, 32) + 2) * 4;
   }
