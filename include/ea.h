@@ -764,10 +764,8 @@ typedef struct {
  * sequence s, at position p = kv_len[s] - rows + r, attends with every head to
  * the tokens j <= p of its sequence; a token's key is its whole row, its value
  * its latent.  Sums and softmax statistics are 32 bits; the weights that
- * multiply the latents are rounded to 11 bits beside f16 and fp8 latents, and
- * beside bf16 ones to 16 bits in calls of up to 64 rows times heads a sequence
- * (max_rows * q_heads), to 8 in others.  A row that attends to nothing gets
- * zeros.  What lies in tokens that a row does not attend to never reaches it.
+ * multiply the latents are rounded to 11 bits beside f16 and fp8 latents, to 8
+ * beside bf16 ones.  A row that attends to nothing gets zeros.  What lies in tokens that a row does not attend to never reaches it.
  * workspace: as for ea_attend, ea_attend_latent_workspace bytes. */
 int64_t ea_attend_latent_workspace(const ea_cache *cache, const ea_batch *batch,
                                    const ea_latent_attention *args);

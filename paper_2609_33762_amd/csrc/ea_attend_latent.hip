@@ -168,7 +168,6 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   constexpr int DT = CT / 32, VB = 8 / EB;      // tiles of O; of them in 16 pieces
   constexpr int AHEAD = 4, VAHEAD = 3;   // reads of keys, values ahead of their use
   constexpr int PV = FP8 ? kF16 : ACT;
-  constexpr bool HILO = PV == kBf16 && QW < 4;
   constexpr float kShift = PV == kF16 ? 7.f : 0.f, kSlack = 8.f;
   constexpr int LPR = RC / 16, RPI = kLanes / LPR, NI = 8 / RPI;  // loads of 8 tokens' latents
   constexpr int EIGHTS = 4 / QW;         // eights of tokens that a wave loads in a step
@@ -539,7 +538,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const float of_score = FP8 ? 1.f : a.scale_log2;
   float top, f, ref;
   uint64_t jump = 0;
-  u32x4 ph[2], pl[2];
+  u32x4 ph[2];
   auto weigh = [&](int i) {
     if (i == 0 || i == 1) {
       float t = kNegInf;
@@ -568,11 +567,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
         l += p;
         if constexpr (FP8) p *= vs[2 * j + part];
       } else {
-        const uint32_t hi = pack_act<PV>(y[2 * j], y[2 * j + 1]);
-        ph[j >> 2][j & 3] = hi;
-        if constexpr (HILO)
-          pl[j >> 2][j & 3] = pack_act<kBf16>(y[2 * j] - __uint_as_float(hi << 16),
-                                              y[2 * j + 1] - __uint_as_float(hi & 0xffff0000u));
+        ph[j >> 2][j & 3] = pack_act<PV>(y[2 * j], y[2 * j + 1]);
       }
     }
   };
@@ -597,7 +592,6 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
         af = u32x4{v.w[0][0], v.w[0][1], v.w[1][0], v.w[1][1]};
       f32x16 &to = o[tile_of_sum(n)];
       to = mfma32<PV>(af, ph[half], to);
-      if constexpr (HILO) to = mfma32<PV>(af, pl[half], to);
       side(n);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -910,14 +904,11 @@ void go(void (*kernel)(LatentAttendArgs), const LatentAttendArgs &a, hipStream_t
 
 template <int ACT, bool FP8, int CT, Mode MODE>
 hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
-  switch (a.wave_columns) {
-    case 1:  // (two steps of 16-bit tokens would not fit)
-      if constexpr (FP8) go(attend_latent<ACT, FP8, CT, 1, MODE>, a, s);
-      else return hipErrorInvalidValue;
-      break;
-    case 2: go(attend_latent<ACT, FP8, CT, 2, MODE>, a, s); break;
-    default: go(attend_latent<ACT, FP8, CT, 4, MODE>, a, s);
+  if constexpr (FP8) {
+    if (a.wave_columns == 1) go(attend_latent<ACT, true, CT, 1, MODE>, a, s);
+    if (a.wave_columns == 2) go(attend_latent<ACT, true, CT, 2, MODE>, a, s);
   }
+  if (a.wave_columns == 4) go(attend_latent<ACT, FP8, CT, 4, MODE>, a, s);
   if (a.slices > 0)
     hipLaunchKernelGGL(join_latent<ACT>,
                        dim3((unsigned)a.b.n_seqs * a.tiles_most * a.wave_columns * a.slices),

@@ -28,14 +28,14 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *
   Parts p{};
   const int64_t most = (int64_t)b->max_rows * a->q_heads;
   const int cus = compute_units(ea::cache_device(c));
-  const int least = ea::cache_desc(c).elem_bytes == 1 ? 1 : 2;
-  p.wave_columns = most <= 32 ? least : most <= 64 ? 2 : 4;
+  const bool fp8 = ea::cache_desc(c).elem_bytes == 1;
+  p.wave_columns = !fp8 || most > 64 ? 4 : most > 32 ? 2 : 1;
   p.wave_columns = env("EA_QW", p.wave_columns);
   const int64_t tile = 32 * p.wave_columns;
   p.tiles = (int32_t)((most + tile - 1) / tile);
   const int64_t units = std::min<int64_t>((int64_t)b->n_seqs * p.tiles,
                                           (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
-  p.wgs = units <= cus ? cus : 2 * cus;
+  p.wgs = units <= cus ? env("EA_WGS",cus) : 2 * cus;
   p.least_steps = units <= cus ? env("EA_LEAST", 4) : units < p.wgs ? 16 : 0;
   const int64_t step = ea::latent_step(p.wave_columns);
   const int64_t steps = (b->max_kv + step - 1) / step;

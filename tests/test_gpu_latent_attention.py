@@ -21,11 +21,9 @@ def kind_args(kind):
 
 
 def weights_of(kind, st):
-    """Rounding of the weights: 11 bits beside f16 and fp8 latents, 16 or 8
-    beside bf16 ones."""
-    if kind != "bf16":
-        return 2.0 ** -11
-    return 2.0 ** -15 if max(st.rows) * st.H <= 64 else 2.0 ** -8
+    """Rounding of the weights: 11 bits beside f16 and fp8 latents, 8 beside
+    bf16 ones."""
+    return 2.0 ** -8 if kind == "bf16" else 2.0 ** -11
 
 
 def attend(st, q, out=None, scale=None):
@@ -129,7 +127,7 @@ def test_strides():
     out = torch.empty((6, st.n_rows, 256), dtype=BF16, device="cuda").transpose(0, 1)
     lse = torch.empty((st.n_rows, 6), device="cuda")
     st.handle.attend_latent(st.layer, st.batch, wide.cuda()[:, 3:9, 8:328], out, scale=0.1, lse=lse)
-    check_attention(st, q, out, lse, 0.1, 2.0 ** -15)
+    check_attention(st, q, out, lse, 0.1, 2.0 ** -8)
 
 
 @pytest.mark.parametrize("page", [16, 5])
@@ -145,8 +143,7 @@ def test_pages_outside_the_cache_hold_no_tokens(rows, heads, page):
     lse = torch.empty((rows, heads), device="cuda")
     st.handle.attend_latent(st.layer, b, q.cuda(), out, scale=0.08, lse=lse)
     hidden = [p * page + i for p in (2, 4) for i in range(page)]
-    check_attention(st, q, out, lse, 0.08, 2.0 ** -15 if rows * heads <= 64 else 2.0 ** -8,
-                    hidden=hidden)
+    check_attention(st, q, out, lse, 0.08, 2.0 ** -8, hidden=hidden)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp8"])
