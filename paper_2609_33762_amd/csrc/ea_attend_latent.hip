@@ -64,19 +64,18 @@ __device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" : : : 
 // A product into vector registers: the sums of O take the accumulation
 // registers, and the compiler puts results of its own matrix instructions there.
 // It does not know what these are, so they bring the waits that the hardware asks
-// for: NOP two cycles after a vector instruction has written an operand, sixteen
+// for: two cycles after a vector instruction may have written an operand, sixteen
 // before one reads the results (settled()).  ZERO: not added to anything.
-template <int ACT, bool ZERO, bool NOP>
+template <int ACT, bool ZERO>
 __device__ inline void multiply32(f32x16 &x, const u32x4 &v, const u32x4 &w) {
-  if constexpr (NOP) asm volatile("s_nop 1");
   if constexpr (ACT == kBf16 && ZERO)
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
   else if constexpr (ACT == kBf16)
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
   else if constexpr (ZERO)
-    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(x) : "v"(v), "v"(w));
   else
-    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(x) : "v"(v), "v"(w));
 }
 __device__ inline void settled(f32x16 &x) { asm volatile("s_nop 15" : "+v"(x)); }
 
@@ -477,9 +476,9 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
                           fp8_pair<ACT, false>(v[1]), fp8_pair<ACT, true>(v[1])};
         const u32x4 hi = {fp8_pair<ACT, false>(v[2]), fp8_pair<ACT, true>(v[2]),
                           fp8_pair<ACT, false>(v[3]), fp8_pair<ACT, true>(v[3])};
-        if (i == 0) multiply32<ACT, true, true>(x, lo, qreg[2 * key_of(i)]);
-        else multiply32<ACT, false, true>(x, lo, qreg[2 * key_of(i)]);
-        multiply32<ACT, false, true>(x, hi, qreg[2 * key_of(i) + 1]);
+        if (i == 0) multiply32<ACT, true>(x, lo, qreg[2 * key_of(i)]);
+        else multiply32<ACT, false>(x, lo, qreg[2 * key_of(i)]);
+        multiply32<ACT, false>(x, hi, qreg[2 * key_of(i) + 1]);
         if (i == KR - 1) {
           settled(x);
 #pragma unroll
@@ -490,8 +489,8 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
           }
         }
       } else {
-        if (i == 0) multiply32<ACT, true, true>(x, v, qreg[key_of(i)]);
-        else multiply32<ACT, false, false>(x, v, qreg[key_of(i)]);
+        if (i == 0) multiply32<ACT, true>(x, v, qreg[key_of(i)]);
+        else multiply32<ACT, false>(x, v, qreg[key_of(i)]);
       }
       side(i);
       __builtin_amdgcn_sched_barrier(0);

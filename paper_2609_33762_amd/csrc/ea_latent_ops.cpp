@@ -23,27 +23,25 @@ struct Parts {
   int64_t unit_bytes, bytes;
 };
 
-static int env(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
 Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *a) {
   Parts p{};
   const int64_t most = (int64_t)b->max_rows * a->q_heads;
   const int cus = compute_units(ea::cache_device(c));
   const bool fp8 = ea::cache_desc(c).elem_bytes == 1;
   p.wave_columns = !fp8 || most > 64 ? 4 : most > 32 ? 2 : 1;
-  p.wave_columns = env("EA_QW", p.wave_columns);
   const int64_t tile = 32 * p.wave_columns;
   p.tiles = (int32_t)((most + tile - 1) / tile);
   const int64_t units = std::min<int64_t>((int64_t)b->n_seqs * p.tiles,
                                           (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
-  p.wgs = units <= cus ? env("EA_WGS",cus) : 2 * cus;
-  p.least_steps = units <= cus ? env("EA_LEAST", 4) : units < p.wgs ? 16 : 0;
+  p.wgs = units <= cus ? cus : 2 * cus;
+  p.least_steps = units <= cus ? 4 : units < p.wgs ? 16 : 0;
   const int64_t step = ea::latent_step(p.wave_columns);
   const int64_t steps = (b->max_kv + step - 1) / step;
   const int64_t whole = p.least_steps ? (steps + p.least_steps - 1) / p.least_steps : 1;
   p.grid = (int32_t)std::min<int64_t>(p.wgs + units, units * whole);
   if (p.grid > units) {
     const int64_t groups = (int64_t)b->n_seqs * p.tiles * p.wave_columns;
-    p.slices = (int32_t)std::min<int64_t>(16, std::max<int64_t>(1, env("EA_SL",256) / groups));
+    p.slices = (int32_t)std::min<int64_t>(16, std::max<int64_t>(1, 256 / groups));
     p.unit_bytes = up((int64_t)b->n_seqs * p.tiles * 8, 16);
     p.bytes = p.unit_bytes + (int64_t)p.grid * tile * (up(a->latent_dim, 32) + 2) * 4;
   }
