@@ -765,8 +765,12 @@ typedef struct {
  * the tokens j <= p of its sequence; a token's key is its whole row, its value
  * its latent.  Sums and softmax statistics are 32 bits; the weights that
  * multiply the latents are rounded to 11 bits beside f16 and fp8 latents, to 8
- * beside bf16 ones.  A row that attends to nothing gets zeros.  What lies in tokens that a row does not attend to never reaches it.
- * workspace: as for ea_attend, ea_attend_latent_workspace bytes. */
+ * beside bf16 ones.  A row that attends to nothing gets zeros.  What lies in
+ * tokens that a row does not attend to never reaches it.
+ *
+ * workspace: ea_attend_latent_workspace bytes (0: may be NULL), 16-byte aligned
+ * device memory that a call writes before it reads: nothing in it has to be
+ * cleared or kept.  Calls that may run at the same time need one each. */
 int64_t ea_attend_latent_workspace(const ea_cache *cache, const ea_batch *batch,
                                    const ea_latent_attention *args);
 int ea_attend_latent(ea_cache *cache, int32_t layer, const ea_batch *batch,
