@@ -803,21 +803,20 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   }
 }
 
-// Joins the parts of a unit's 32 rows, some tiles of 32 elements:
+// Joins the parts of a unit's 32 rows, some pieces (a quarter of a tile's 32
+// elements) of them:
 //   o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i,  m = max_i m_i.
 // A launch of its own, so that many workgroups read the parts and nothing waits
-// or counts.  First all parts' factors, 32 rows at a time; then wave (g, i4) adds
-// a quarter of a tile's elements of every kGroups-th part.
-constexpr int kGroups = 4, kJoinThreads = kGroups * 4 * kLanes;
-constexpr int kFactors = 512;  // parts whose factors fit
+// or counts.  A wave runs once over a piece's parts, kAhead at a time, with the
+// running reference and sums of a softmax; where there are many, over every
+// kGroups-th, and then the waves' become one.
+constexpr int kGroups = 8, kJoinThreads = kGroups * kLanes, kAhead = 8;
 template <int ACT>
 __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) {
-  constexpr int TOGETHER = kJoinThreads / 32;
-  __shared__ float factor[kFactors][32];
-  __shared__ float each[2][TOGETHER][32];
-  __shared__ f32x4 sums[kGroups][4][kLanes];
-  const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
-  const int wave = uniform(tid >> 6), i4 = wave & 3, g = wave >> 2;
+  __shared__ f32x4 sums[kGroups][kLanes];
+  __shared__ f32x2 stats[kGroups][kLanes];
+  const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+  const int g = uniform((int)threadIdx.x >> 6);
   const int QW = a.wave_columns, HQ = a.q_heads, C = a.latent, cols = (C + 31) & ~31;
   uint32_t u = blockIdx.x;
   const int slice = u % a.slices;
@@ -829,71 +828,77 @@ __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) 
   const int r = tile * QW * 32 + qg * 32 + c, rows_all = sq.rows * HQ;
   if (r - c >= rows_all) return;
   const int w0 = a.units[2 * ((int64_t)s * a.tiles_most + tile)];
-  const int parts = min(a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1], kFactors);
+  const int parts = a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1];
   if (parts <= 1) return;
-  const bool mine = r < rows_all;
   const int64_t pitch = (int64_t)(QW * 32) * (cols + 2);
   const float *first = a.parts + (int64_t)w0 * pitch;
-  {
-    const int k0 = tid >> 5;
-    const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);
-    f32x2 v[kFactors / TOGETHER];
-    float ref = kNegInf, total = 0.f;
-#pragma unroll
-    for (int i = 0; i < kFactors / TOGETHER; ++i) {
-      v[i] = f32x2{kNegInf, 0.f};
-      if (mine && k0 + i * TOGETHER < parts)
-        v[i] = *reinterpret_cast<const f32x2 *>(ml + (k0 + i * TOGETHER) * pitch);
-    }
-#pragma unroll
-    for (int i = 0; i < kFactors / TOGETHER; ++i) ref = fmaxf(ref, v[i][0]);
-    each[0][k0][c] = ref;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < TOGETHER; ++i) ref = fmaxf(ref, each[0][i][c]);
-    const float zero = ref == kNegInf ? 0.f : ref;
-#pragma unroll
-    for (int i = 0; i < kFactors / TOGETHER; ++i) {
-      if (k0 + i * TOGETHER >= parts) break;
-      const float f = exp2_fast(v[i][0] - zero);
-      total += f * v[i][1];
-      factor[k0 + i * TOGETHER][c] = f;
-    }
-    each[1][k0][c] = total;
-    __syncthreads();
-    total = 0.f;
-#pragma unroll
-    for (int i = 0; i < TOGETHER; ++i) total += each[1][i][c];
-    if (mine && slice == 0 && wave == 0 && h == 0 && a.lse)
-      a.lse[(int64_t)(sq.row0 + r / HQ) * HQ + r % HQ] =
-          total == 0.f ? kNegInf : (ref + __log2f(total)) * 0.6931471805599453f;
-    const float norm = total == 0.f ? 0.f : 1.f / total;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kFactors / TOGETHER; ++i)
-      if (k0 + i * TOGETHER < parts) factor[k0 + i * TOGETHER][c] *= norm;
-    __syncthreads();
-  }
-  uint16_t *out = a.out.data + (int64_t)(sq.row0 + r / HQ) * a.out.row_stride +
-                  (int64_t)(r % HQ) * a.out.head_stride;
-  for (int dt = slice; dt < cols / 32; dt += a.slices) {
-    const int d = dt * 32 + i4 * 8 + h * 4;
+  const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);
+  const bool alone = parts <= 2 * kAhead;
+  const int k_first = alone ? 0 : g, k_step = alone ? 1 : kGroups;
+  const int pieces = a.slices * (alone ? kGroups : 1);
+  for (int piece = alone ? slice * kGroups + g : slice; piece < cols / 8; piece += pieces) {
+    const int d = piece * 8 + h * 4;
+    const bool mine = r < rows_all && d < C;
+    const float *p = first + qg * 32 * cols + (piece * kLanes + lane) * 4;
+    float m = kNegInf, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (mine && d < C) {
-      const float *p = first + qg * 32 * cols + ((dt * 4 + i4) * kLanes + lane) * 4;
-#pragma unroll 8
-      for (int k = g; k < parts; k += kGroups)
-        acc += factor[k][c] * *reinterpret_cast<const f32x4 *>(p + k * pitch);
-    }
-    sums[g][i4][lane] = acc;
-    __syncthreads();
-    if (g == 0 && mine && d < C) {
+    for (int k0 = k_first; k0 < parts; k0 += k_step * kAhead) {
+      f32x2 of[kAhead];
+      f32x4 v[kAhead];
 #pragma unroll
-      for (int k = 1; k < kGroups; ++k) acc += sums[k][i4][lane];
-      *reinterpret_cast<u32x2 *>(out + d) =
-          u32x2{pack_act<ACT>(acc[0], acc[1]), pack_act<ACT>(acc[2], acc[3])};
+      for (int i = 0; i < kAhead; ++i) {
+        const int k = k0 + i * k_step;
+        of[i] = f32x2{kNegInf, 0.f};
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (mine && k < parts) {
+          of[i] = *reinterpret_cast<const f32x2 *>(ml + k * pitch);
+          v[i] = *reinterpret_cast<const f32x4 *>(p + k * pitch);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) top = fmaxf(top, of[i][0]);
+      const float ref = top == kNegInf ? 0.f : top, f = exp2_fast(m - ref);
+      m = top;
+      l *= f;
+      acc *= f;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const float w = exp2_fast(of[i][0] - ref);
+        l += w * of[i][1];
+        acc += w * v[i];
+      }
     }
-    __syncthreads();
+    if (!alone) {
+      sums[g][lane] = acc;
+      stats[g][lane] = f32x2{m, l};
+      __syncthreads();
+      if (g == 0) {
+        m = kNegInf;
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) m = fmaxf(m, stats[k][lane][0]);
+        const float ref = m == kNegInf ? 0.f : m;
+        l = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+          const float w = exp2_fast(stats[k][lane][0] - ref);
+          l += w * stats[k][lane][1];
+          acc += w * sums[k][lane];
+        }
+      }
+      __syncthreads();
+    }
+    if (mine && (alone || g == 0)) {
+      const float norm = l == 0.f ? 0.f : 1.f / l;
+      const int64_t row = sq.row0 + r / HQ, head = r % HQ;
+      *reinterpret_cast<u32x2 *>(a.out.data + row * a.out.row_stride + head * a.out.head_stride +
+                                 d) =
+          u32x2{pack_act<ACT>(acc[0] * norm, acc[1] * norm),
+                pack_act<ACT>(acc[2] * norm, acc[3] * norm)};
+      if (d == 0 && a.lse)
+        a.lse[row * HQ + head] = l == 0.f ? kNegInf : (m + __log2f(l)) * 0.6931471805599453f;
+    }
   }
 }
 
