@@ -28,11 +28,22 @@ Parts parts_of(const ea_cache *c, const ea_batch *b, const ea_latent_attention *
   const int64_t most = (int64_t)b->max_rows * a->q_heads;
   const int cus = compute_units(ea::cache_device(c));
   const bool fp8 = ea::cache_desc(c).elem_bytes == 1;
+  // As few waves on other columns of the same tokens as hold the rows times heads:
+  // 64 sequences of 8,192-65,536 tokens in fp8, 16 columns: 1, 2, 4 waves 336, 578,
+  // 755 us; 64 columns: 2, 4 waves 608, 787; 128 columns: 2, 4 waves 1676, 848.  In
+  // 16 bits two waves on the same tokens leave a tile no registers for the queries (24
+  // sequences of 2-4 rows of 16 heads: 126 us, with four 101).
   p.wave_columns = !fp8 || most > 64 ? 4 : most > 32 ? 2 : 1;
   const int64_t tile = 32 * p.wave_columns;
   p.tiles = (int32_t)((most + tile - 1) / tile);
   const int64_t units = std::min<int64_t>((int64_t)b->n_seqs * p.tiles,
                                           (int64_t)b->n_rows * a->q_heads / tile + b->n_seqs);
+  // A workgroup has a compute unit to itself.  Fewer units than those: one part for
+  // each (64 sequences, fp8: 308 us; 1.5 or 2 parts for each: 382, 335), of four steps at
+  // least (16: 29 us in place of 18 for 512 tokens, as much for 65,536; 2: 109 in place
+  // of 102 for 24 sequences).  Up to twice as many: long ones are split, so that no compute unit
+  // gets two of them (300 sequences of 500-16,000 tokens: 387 us, whole 426, four
+  // times as many parts 410; bf16: 848, 1000, 817).  More: whole units, one launch.
   p.wgs = units <= cus ? cus : 2 * cus;
   p.least_steps = units <= cus ? 4 : units < p.wgs ? 16 : 0;
   const int64_t step = ea::latent_step(p.wave_columns);

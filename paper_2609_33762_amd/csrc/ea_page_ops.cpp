@@ -105,6 +105,9 @@ int ea_move_tokens(ea_cache *c, const ea_cache_planes *planes, int32_t layer_beg
   const int64_t unit = latents && d.elem_bytes == 2 ? 16 : T;
   k.blocks_most = (int32_t)((a->max_tokens + unit - 1) / unit);
   const int64_t blocks = (int64_t)a->n_seqs * k.blocks_most;
+  // As many layers as leave 8,192 waves, since lookups and angles serve all of them: two
+  // layers of 16 and of 8 long contexts 420 and 205 us, one at a time 440 and 244; of
+  // one short context 5.0 us one at a time, both 6.7.
   k.layers_wave = (int32_t)std::min<int64_t>(
       layer_count, std::max<int64_t>(1, blocks * layer_count / 8192));
   k.latent = a->latent_dim;
