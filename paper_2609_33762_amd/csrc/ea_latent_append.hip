@@ -182,7 +182,10 @@ __device__ inline int32_t sequence_of_row_wave(const BatchRows &b, int32_t row) 
   return lo;
 }
 
-constexpr int kRowPieces = 4 * kLanes;  // pieces of a row's queries that a wave rotates
+// Heads of a row's queries that a wave rotates, and rotates at once: whole ones, as
+// q_out may be q and a head's halves turn together.
+__host__ __device__ inline int heads_at_once(int per) { return kLanes / per; }
+__host__ __device__ inline int heads_of_wave(int per) { return 4 * heads_at_once(per); }
 
 template <int ACT, bool FP8>
 __global__ __launch_bounds__(kThreads) void append_latent(LatentAppendArgs a, uint32_t blocks) {
@@ -216,8 +219,8 @@ __global__ __launch_bounds__(kThreads) void append_latent(LatentAppendArgs a, ui
     return;
   }
   // ---- queries
-  const int lane = threadIdx.x & 63, per = R >> 3, pieces = a.q_heads * per;
-  const int waves = (pieces + kRowPieces - 1) / kRowPieces;
+  const int lane = threadIdx.x & 63, per = R >> 3, once = heads_at_once(per);
+  const int wave_heads = heads_of_wave(per), waves = (a.q_heads + wave_heads - 1) / wave_heads;
   const uint32_t u = (blockIdx.x - blocks) * kWaves + uniform((int)threadIdx.x >> 6);
   const int row = u / waves;
   if (row >= a.b.n_rows) return;
@@ -225,10 +228,11 @@ __global__ __launch_bounds__(kThreads) void append_latent(LatentAppendArgs a, ui
   const Seq sq = sequence(a.b, s);
   const int pos = sq.len - sq.rows + row - sq.row0;
   if (row < sq.row0 || row >= sq.row0 + sq.rows || pos < 0) return;
-  const int from = (u % waves) * kRowPieces;
+  const int h0 = lane / per, rp = lane - h0 * per, from = (u % waves) * wave_heads;
+  const int to = min(from + wave_heads, a.q_heads);
+  if (h0 >= once) return;
 #pragma unroll 4
-  for (int at = from + lane; at < min(from + kRowPieces, pieces); at += kLanes) {
-    const int h = at / per, rp = at - h * per;
+  for (int h = from + h0; h < to; h += once) {
     const uint16_t *src = a.q.data + row * a.q.row_stride + h * a.q.head_stride;
     float x[8];
     read8<ACT>(src + rp * 8, x);
@@ -481,7 +485,8 @@ hipError_t append(const LatentAppendArgs &a, hipStream_t s) {
   const int64_t blocks = (int64_t)a.b.n_seqs * a.pages_most;
   int64_t grid = blocks;
   if (a.q.data) {
-    const int64_t waves = ((int64_t)a.q_heads * (a.turn / 8) + kRowPieces - 1) / kRowPieces;
+    const int most = heads_of_wave(a.turn / 8);
+    const int64_t waves = ((int64_t)a.q_heads + most - 1) / most;
     grid += (a.b.n_rows * waves + kWaves - 1) / kWaves;
   }
   hipLaunchKernelGGL((append_latent<ACT, FP8>), dim3((unsigned)grid), dim3(kThreads), 0, s, a,

@@ -110,7 +110,7 @@ int ea_append_latent(ea_cache *c, int32_t layer, const ea_batch *b, const ea_lat
   k.pages_most = (int32_t)((b->max_rows + (int64_t)d.page_tokens - 2) / d.page_tokens + 1);
   // workgroups, and waves of queries, are counted in 32 bits
   const int64_t blocks = (int64_t)b->n_seqs * k.pages_most;
-  const int64_t queries = (int64_t)b->n_rows * ((int64_t)k.q_heads * k.turn / 2048 + 1);
+  const int64_t queries = (int64_t)b->n_rows * ((int64_t)k.q_heads * k.turn / 1920 + 1);
   if (blocks > INT32_MAX / 2 || queries > INT32_MAX / 2) return EA_ENOTSUP;
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());

@@ -427,3 +427,17 @@ def test_appended_without_angles_and_queries_in_place():
     pos = torch.tensor([17, 18, 19, 0, 1, 2, 3, 4])
     want, mag = turn64(q0, rope, pos, False)
     assert ((q.cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -22 * mag).all()
+
+
+@pytest.mark.parametrize("turn", [16, 32, 48, 64])
+@pytest.mark.parametrize("heads", [11, 24, 128])
+def test_queries_of_many_heads_in_place(turn, heads):
+    # heads whose pieces are no whole part of a wave's lanes
+    need_gpu()
+    st = Latents(kv_lens=[20, 5, 70], rows=[3, 5, 1], heads=heads, latent=128, turn=turn)
+    both, q = st.rand(9, 1, 128 + turn).cuda(), st.rand(9, heads, turn).cuda()
+    rope, q0 = angles(70, turn), q.cpu()
+    st.handle.append_latent(st.layer, st.batch, both[..., :128], both[..., 128:], rope=rope.cuda(),
+                            q=q, q_out=q)
+    want, mag = turn64(q0, rope, torch.tensor([17, 18, 19, 0, 1, 2, 3, 4, 69]), False)
+    assert ((q.cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -22 * mag).all()

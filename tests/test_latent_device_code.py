@@ -160,7 +160,7 @@ def kernels(text):
         yield name, Code(body.split("\n"))
 
 
-def test_the_checker_sees_missing_waits():
+def test_missing_waits_are_seen():
     mfma = "\tv_mfma_f32_32x32x16_bf16 v[0:15], v[16:19], v[20:23], 0\n"
     lines = lambda s: hazards(Code(s.split("\n")))  # noqa: E731
     assert lines(mfma + "\tv_mov_b32_e32 v30, v3\n")
