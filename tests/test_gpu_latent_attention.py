@@ -193,3 +193,21 @@ def test_scales_of_blocks_of_zeros():
     q = st.rand(2, 16, 576)
     out, lse, scale = attend(st, q)
     check_attention(st, q, out, lse, scale, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("n,most,heads", [(70, 900, 3), (270, 500, 2), (300, 1300, 33), (530, 200, 2)])
+def test_many_sequences(n, most, heads, kind):
+    # more than a wave's lanes; more units than compute units, whole or in parts
+    lens = [(i * 37) % most for i in range(n)]
+    lens[n // 2], lens[n - 1] = most, 2 * most
+    case(kind, kv_lens=lens, rows=[1 + (i % 7 == 0) for i in range(n)], heads=heads, latent=64,
+         turn=16)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("length", [129, 1000, 2100, 9000])
+@pytest.mark.parametrize("latent", [16, 48, 512])
+def test_parts_of_one_sequence(length, latent, kind):
+    # two parts, some, as many as one wave joins, and more
+    case(kind, kv_lens=[length], rows=[1], heads=6, latent=latent, turn=16)
