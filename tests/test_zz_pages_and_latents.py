@@ -10,7 +10,7 @@ from gpu_common import need_gpu
 from latent_common import BF16, F16, Latents, check_attention
 from paper_2609_33762_amd import _native as N
 from paper_2609_33762_amd import api
-from test_gpu_page_moves import Moved, angles, turn64
+from test_zz_pages_moves import Moved, angles, turn64
 
 pytestmark = pytest.mark.gpu
 
