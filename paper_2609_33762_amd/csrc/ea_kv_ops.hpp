@@ -111,7 +111,7 @@ struct LatentAttendArgs {
   int32_t wave_columns, tiles_most;
   int32_t split_wgs, least_steps, split_grid;
   int32_t *units;           // [n_seqs][tiles_most][2]: a unit's first workgroup, its parts
-  float *parts;             // [split_grid][32 * wave_columns][latent + 2]
+  float *parts;             // [split_grid][32 * wave_columns][latent, whole 32, + 2]
   int32_t slices;           // workgroups that join a unit's 32 rows; 0: nothing is split
 };
 

@@ -8,7 +8,7 @@
 // of a token each, side by side over the block, and keeps them in registers between
 // the search for the largest value and the rounding, so that each is read once.
 // Queries go by waves of the same launch.  Measured: 5 ragged pieces of prompts, fp8,
-// 54 MB: 15-17 us (3.3 TB/s; launch and the search 4 of them); 4 tokens: 3.7 us.
+// 54 MB: 15-17 us (3.3 TB/s); 4 tokens: 3.7 us.
 // Moved 16-bit latents, 953 MB: 205 us (4.6 TB/s); with latents unpacked and packed
 // again as their turned parts are 277.
 #include <hip/hip_runtime.h>

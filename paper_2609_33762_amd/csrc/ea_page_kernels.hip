@@ -12,8 +12,8 @@
 // Moves: a wave takes a block's 16 tokens, whose places and angles it looks up once
 // for all heads and several layers.  16 contexts of 8,192-65,536 tokens, fp8 with
 // bounds, two layers, 1.71 GB: 420 us (4.06 TB/s); a wave for each head and layer,
-// with the lookups each time: 1,902 us.  What is left is the search for a block's
-// largest value and the rounding, a quarter of the time beside the reading.
+// with the lookups each time: 1,902 us.  Beside the reading a wave decodes, searches a
+// block's largest value, rounds and makes bounds: 15% below the copies' rate.
 #include <hip/hip_runtime.h>
 
 #include "ea_kv_blocks.hpp"
