@@ -14,17 +14,18 @@
 // first product as the second one's operand takes them, without a way through LDS.
 // A workgroup is one wave for each SIMD, which has its 512 registers: 32 columns'
 // queries (144) and sums (256, in the accumulation registers), of 512 elements.  So
-// a tile of rows is read from LDS once for each 32 columns.  Rows go to LDS as they are stored, by loads that write no register; keys are
-// read in rows, values with transposing reads, of places swapped so that no two
-// lanes meet in a bank (counted: no conflicts).
+// a tile of rows is read from LDS once for each 32 columns.  Rows go to LDS as they
+// are stored, by loads that write no register; keys are read in rows, values with
+// transposing reads, of places swapped so that no two lanes meet in a bank
+// (counted: no conflicts).
 //
 // The reference m of a row moves only when a score is more than 2^8 above it, so
 // the sums are rarely rescaled; statistics and sums have 32 bits.  Weights are
 // rounded to 11 bits beside f16 and fp8 values (up to 2^15: 7 of shift, 8 of
 // slack), to 8 beside bf16 ones, as the products bound the kernel there: half a
-// step, 2^-8, of each, of random signs in a sum, as the result's own rounding is;
-// a second bf16 for the rest would make half of the products anew.  An fp8 value's scale goes into its
-// weight before that.
+// step, 2^-8, of each, of random signs in a sum, as the result's own rounding is; a
+// second bf16 for the rest would make half of the products anew.  An fp8 value's
+// scale goes into its weight before that.
 //
 // Measured (C 512, R 64, pages of 16 tokens in random order), the join included:
 // 64 sequences of 8,192-65,536 tokens, a row of 16 heads, fp8: 305 us (4.6 TB/s; its

@@ -3,11 +3,11 @@ definition in 64 bits; latents appended.
 
 A moved or appended key passes through two products and a sum in 32 bits, of
 magnitudes |x_i| + |x_j| (2^-22 of them), and one rounding: to 16 bits u = 2^-8
-(bf16) or 2^-11 (f16) of the value (f16 values below 2^-14 are 2^-24 apart: off by up
-to 2^-25, more than 2^-11 of a value below 2^-14; bf16 has the exponents of 32 bits), to fp8 2^-4 of it or half the smallest
-subnormal, 2^-10, times the block's scale.  Scales are the smallest powers of
-two that hold their block; values, 16-bit ones and those that need no new
-rounding, are exact."""
+(bf16) or 2^-11 (f16) of the value (f16 values below 2^-14 are 2^-24 apart: off by
+up to 2^-25, more than 2^-11 of a value below 2^-14; bf16 has the exponents of 32
+bits), to fp8 2^-4 of it or half the smallest subnormal, 2^-10, times the block's
+scale. Scales are the smallest powers of two that hold their block; values, 16-bit
+ones and those that need no new rounding, are exact."""
 import math
 
 import pytest
