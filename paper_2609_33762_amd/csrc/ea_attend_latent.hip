@@ -6,8 +6,9 @@
 //
 // All query heads share a token's row, so the rows of a matrix product are
 // query rows times heads, and a cached byte feeds both products: 2 (2 C + R) H
-// operations for (C + R) e bytes, 30 a byte for each head (C 512, R 64, 16 bits),
-// so that a row of 16 heads is bound by memory and of 128 by the products.
+// operations for (C + R) e bytes, 1.9 a byte for each head (C 512, R 64, 16 bits),
+// so that a row of 16 heads is bound by memory, one of 128 (242 a byte) by both
+// alike, and more rows by the products.
 //
 // Both products are turned around, S^T = K Q^T and O^T = V^T P^T: a column is a
 // row's head, a lane has one column's statistics, and the weights come out of the
