@@ -73,6 +73,16 @@ __device__ inline void fp8_values(uint32_t w, float x[4]) {
   x[3] = b[1];
 }
 
+// What takes codes of scale `by` to those of a new block, 1 / inv its scale: exact,
+// as inv is a power of two.  Beside codes that are all zeros it may pass 32 bits
+// (one that is not gives the new block a scale that keeps it below 2^19), and zeros
+// times infinity are NaN: it stays finite where `by` is.
+__device__ inline float factor_of(float by, float inv) {
+  constexpr float kMost = 0x1.fffffep127f;
+  const float f = by * inv;
+  return finite(by) ? fmaxf(fminf(f, kMost), -kMost) : f;
+}
+
 // Elements d0 .. d0+7 of a stored token as values.
 template <int ACT, bool FP8>
 __device__ inline void stored8(const uint8_t *p, float scale, float x[8]) {

@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void move_tokens(MoveArgs a, uint32_t uni
         }
       }
       auto store = [&](int t, float y[16], float by) {
-        const float f = by * inv;  // exact: inv is a power of two
+        const float f = factor_of(by, inv);
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           if (!at.in[n]) continue;

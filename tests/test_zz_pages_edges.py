@@ -1,0 +1,64 @@
+"""Moved, appended and attended tokens on the GPU where a block, a batch or its
+memory is out of the ordinary."""
+import pytest
+import torch
+
+from gpu_common import need_gpu
+from latent_common import FP8
+from paper_2609_33762_amd import api
+from test_zz_pages_moves import angles
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.as_tensor(x, dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------ fp8 blocks of zeros, moved
+
+def zeros_and_few(where):
+    """Codes of blocks 0 and 1 (zeros), 2 (zeros but where `where` says so), and
+    scales that hold values up to 448 * 2^20, or, of block 2, the least ones."""
+    scales = torch.tensor([4.0, 2.0 ** 20, 2.0 ** -126])
+    codes = torch.zeros((3, *where.shape))
+    codes[2] = where * torch.tensor([1.0, -448.0, 0.5, 2.0 ** -9]).repeat(
+        -(-where.numel() // 4))[:where.numel()].view(where.shape)
+    codes[0].view(-1)[::3] = -0.0
+    return codes.to(FP8), scales
+
+
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("page", [16, 48])
+@pytest.mark.parametrize("dim,pairs", [(64, 64), (128, 128), (256, 256), (72, 72), (64, 20)])
+def test_moved_zeros_stay_zeros(dim, pairs, page, turned):
+    # a factor from an old block's scale to a new one's may pass 32 bits where all
+    # codes are zeros; tokens of such blocks alone, and beside very small ones
+    need_gpu()
+    heads = 2
+    where = (torch.arange(page) % 2 == 0)[:, None, None] * torch.ones(heads, dim)
+    codes, scales = zeros_and_few(where)
+    kv = torch.zeros((1, 8, 2, page, heads, dim), dtype=FP8)
+    kv[0, :3] = codes[:, None].expand(3, 2, page, heads, dim)
+    plane = torch.ones((1, 8, 2, heads))
+    plane[0, :3] = scales[:, None, None]
+    d_kv, d_plane = kv.cuda(), plane.cuda()
+    bounds = torch.full((1, 8, 2, heads, dim), 77, dtype=torch.int8, device="cuda")
+    unit = torch.full((1, 8, heads), 7.0, device="cuda")
+    cache = api.Cache(d_kv, 8, 1, page, heads, dim, 1, head_scales=d_plane, bounds=bounds,
+                      bound_scales=unit)
+    # new block 4: zeros of both kinds; 5: of the second kind beside the small values
+    half = page // 2
+    tokens = list(range(half)) + list(range(page, page + half)) + \
+        list(range(page + half, 2 * page)) + list(range(2 * page, 2 * page + half))
+    rope = angles(3 * page, pairs).cuda() if turned else None
+    cache.move_tokens(ints([[0, 1, 2]]), ints([[4, 5]]), ints(tokens), ints([0, len(tokens)]),
+                      max_tokens=len(tokens), max_kv=3 * page, rope=rope)
+    got, sc = d_kv.cpu().float(), d_plane.cpu()
+    assert (got[0, 4] == 0).all()
+    assert (sc[0, 4] == 2.0 ** -126).all()
+    assert (bounds[0, 4] == 0).all()
+    assert (got[0, 5, :, :page - half] == 0).all()
+    small = got[0, 5, :, page - half:page - half + half]
+    assert torch.isfinite(small).all() and (small[:, ::2] != 0).any(-1).all()
+    assert torch.equal(small[1], codes[2, :half].float())  # values, whose scale stays
