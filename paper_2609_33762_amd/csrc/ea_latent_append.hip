@@ -457,7 +457,7 @@ __global__ __launch_bounds__(kThreads) void move_latents(MoveArgs a) {
 #pragma unroll
         for (int k = 0; k < KEEP; ++k) {
           if (dst[k] < 0) continue;
-          const float f = r.lat_scale[k] * inv[0];
+          const float f = factor_of(r.lat_scale[k], inv[0]);
           u32x4 w;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void move_latents(MoveArgs a) {
           *reinterpret_cast<u32x4 *>(base + dst[k]) = w;
         }
         if (tdst >= 0) {
-          const float f = r.turn_scale * inv[1];
+          const float f = factor_of(r.turn_scale, inv[1]);
           float x[8];
           turned(r, x);
           *reinterpret_cast<u32x2 *>(base + tdst) =

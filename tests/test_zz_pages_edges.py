@@ -62,3 +62,31 @@ def test_moved_zeros_stay_zeros(dim, pairs, page, turned):
     small = got[0, 5, :, page - half:page - half + half]
     assert torch.isfinite(small).all() and (small[:, ::2] != 0).any(-1).all()
     assert torch.equal(small[1], codes[2, :half].float())  # values, whose scale stays
+
+
+@pytest.mark.parametrize("latent,turn,page", [(128, 32, 16), (512, 64, 16), (384, 48, 5),
+                                              (256, 64, 40)])
+@pytest.mark.parametrize("turned", [False, True])
+def test_moved_latents_of_zeros_stay_zeros(latent, turn, page, turned):
+    need_gpu()
+    where = (torch.arange(page) % 2 == 0)[:, None] * torch.ones(latent + turn)
+    codes, scales = zeros_and_few(where)
+    kv = torch.zeros((1, 8, page, latent + turn), dtype=FP8)
+    kv[0, :3] = codes
+    plane = torch.ones((1, 8, 2))
+    plane[0, :3] = scales[:, None]
+    d_kv, d_plane = kv.cuda(), plane.cuda()
+    cache = api.LatentCache(d_kv, 8, 1, page, latent, turn, 1, scales=d_plane)
+    half = page // 2
+    tokens = list(range(half)) + list(range(page, page + page - half)) + \
+        list(range(page + half, 2 * page)) + list(range(2 * page, 2 * page + half))
+    rope = angles(3 * page, turn).cuda() if turned else None
+    cache.move_tokens(ints([[0, 1, 2]]), ints([[4, 5]]), ints(tokens), ints([0, len(tokens)]),
+                      max_tokens=len(tokens), max_kv=3 * page, rope=rope)
+    got = d_kv.cpu().float()
+    assert (got[0, 4] == 0).all()
+    assert (d_plane[0, 4] == 2.0 ** -126).all()
+    assert (got[0, 5, :page - half] == 0).all()
+    small = got[0, 5, page - half:page]
+    assert torch.isfinite(small).all()
+    assert torch.equal(small[:, :latent], codes[2, :half, :latent].float())
