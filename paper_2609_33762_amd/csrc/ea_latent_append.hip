@@ -194,6 +194,9 @@ __global__ __launch_bounds__(kThreads) void append_latent(LatentAppendArgs a, ui
   if (blockIdx.x < blocks) {
     const int s = blockIdx.x / a.pages_most, j = blockIdx.x % a.pages_most;
     const Seq sq = sequence(a.b, s);
+    // (nothing of a sequence without rows is read or written: its length and table
+    // may be those of an earlier step, its pages another sequence's by now)
+    if (sq.rows == 0) return;
     const int start = max(sq.len - sq.rows, 0);  // first new position
     const int p = over_page(kv, start) + j;
     if (p * T >= sq.len) return;

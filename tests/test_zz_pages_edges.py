@@ -1,10 +1,12 @@
 """Moved, appended and attended tokens on the GPU where a block, a batch or its
 memory is out of the ordinary."""
+import math
+
 import pytest
 import torch
 
 from gpu_common import need_gpu
-from latent_common import FP8
+from latent_common import FP8, Latents
 from paper_2609_33762_amd import api
 from test_zz_pages_moves import angles
 
@@ -90,3 +92,43 @@ def test_moved_latents_of_zeros_stay_zeros(latent, turn, page, turned):
     small = got[0, 5, page - half:page]
     assert torch.isfinite(small).all()
     assert torch.equal(small[:, :latent], codes[2, :half, :latent].float())
+
+
+# --------------------------------------- sequences without rows in a step
+
+@pytest.mark.parametrize("scale", [math.nan, 0.0, 2.0 ** -140, -1.0, math.inf, 0.375])
+@pytest.mark.parametrize("page", [16, 40])
+def test_appended_latents_of_others_leave_a_sequence_without_rows_alone(page, scale):
+    # its last block is filled in part; whatever its scales are they stay
+    need_gpu()
+    st = Latents([20, 60, 17], [0, 5, 0], heads=2, fp8=True, pow2=True, page=page)
+    mine = [int(st.table[s, 20 // page if s == 0 else 17 // page]) for s in (0, 2)]
+    st.scales[st.layer, mine] = scale
+    st.to_device()
+    new = st.rand(5, 1, 160).cuda()
+    st.handle.append_latent(st.layer, st.batch, new[..., :128], new[..., 128:],
+                            rope=angles(60, 32).cuda())
+    theirs = [int(p) for p in st.table[1] if p >= 0]
+    rest = [p for p in range(st.P) if p not in theirs]
+    for got, was in ((st.d_cache, st.cache), (st.d_scales, st.scales)):
+        assert torch.equal(got.cpu()[:, rest].view(torch.uint8), was[:, rest].view(torch.uint8))
+    assert not torch.equal(st.d_cache.cpu()[:, theirs].view(torch.uint8),
+                           st.cache[:, theirs].view(torch.uint8))
+
+
+def test_appended_latents_take_no_heed_of_a_free_place_s_old_table():
+    # a place of the batch that is free now, its length and table those of an earlier
+    # step: the block that another sequence goes on writing
+    need_gpu()
+    results = []
+    for stale in (False, True):
+        st = Latents([40, 60], [0, 3], heads=2, fp8=True, pow2=True)
+        if stale:
+            st.table[0, 2] = st.table[1, 3]
+        st.scales[st.layer] = 2.0 ** -20  # grows for any new token
+        st.to_device()
+        new = st.rand(3, 1, 160).cuda()
+        st.handle.append_latent(st.layer, st.batch, new[..., :128], new[..., 128:])
+        results.append([t.cpu().view(torch.uint8) for t in (st.d_cache, st.d_scales)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
