@@ -629,7 +629,9 @@ typedef struct {
  * then the older codes are requantised to it.  Values that are not finite
  * become NaN.  With bounds, the touched blocks' bounds are made from all
  * their stored keys.  Pages that get new tokens must belong to one sequence
- * of the batch alone; a prefix shared by several is fine. */
+ * of the batch alone; a prefix shared by several is fine.  Of a sequence without
+ * rows in the step (a free place of a padded batch) nothing is read or written,
+ * whatever its length and table say. */
 int ea_append_kv(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,
                  const ea_batch *batch, const ea_append *args, hipStream_t stream);
 
@@ -739,8 +741,8 @@ typedef struct {
  * values: row r of sequence s goes to position kv_len[s] - rows + r, its latent
  * as it is, its key part rotated in 32 bits and rounded once; q_out gets the
  * rotated parts of the queries.  fp8: the scales of a block's latents and of
- * its key parts follow ea_append_kv's rule.  Pages that get new tokens must
- * belong to one sequence of the batch alone. */
+ * its key parts follow ea_append_kv's rule, and so do sequences without rows.
+ * Pages that get new tokens must belong to one sequence of the batch alone. */
 int ea_append_latent(ea_cache *cache, int32_t layer, const ea_batch *batch,
                      const ea_latent_append *args, hipStream_t stream);
 

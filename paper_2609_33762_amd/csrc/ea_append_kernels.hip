@@ -100,6 +100,9 @@ __device__ inline void append_block(const AppendArgs &a, uint32_t u, int lane) {
   u /= H;
   const int j = u % a.pages_most, s = u / a.pages_most;
   const Seq sq = sequence(a.b, s);
+  // (nothing of a sequence without rows is read or written: its length and table
+  // may be those of an earlier step, its pages another sequence's by now)
+  if (sq.rows == 0) return;
   const int start = max(sq.len - sq.rows, 0);  // first new position
   const int p = over_page(kv, start) + j;
   if (p * T >= sq.len) return;

@@ -8,6 +8,7 @@ import torch
 from gpu_common import need_gpu
 from latent_common import FP8, Latents
 from paper_2609_33762_amd import api
+from test_gpu_cache_ops import Setup
 from test_zz_pages_moves import angles
 
 pytestmark = pytest.mark.gpu
@@ -130,5 +131,48 @@ def test_appended_latents_take_no_heed_of_a_free_place_s_old_table():
         new = st.rand(3, 1, 160).cuda()
         st.handle.append_latent(st.layer, st.batch, new[..., :128], new[..., 128:])
         results.append([t.cpu().view(torch.uint8) for t in (st.d_cache, st.d_scales)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("scale", [math.nan, 0.0, 2.0 ** -140, -1.0, math.inf, 0.375, None])
+@pytest.mark.parametrize("page", [16, 40])
+def test_appended_keys_of_others_leave_a_sequence_without_rows_alone(page, scale):
+    # None: a 16-bit cache; bounds of the block stay too, which may hold more tokens
+    # than an earlier step's length says
+    need_gpu()
+    st = Setup([20, 60, 17], [0, 5, 0], heads=2, dim=64, fp8=scale is not None, bounds=True,
+               page=page)
+    mine = [int(st.table[s, 20 // page if s == 0 else 17 // page]) for s in (0, 2)]
+    if scale is not None:
+        st.scales[st.layer, mine] = scale
+        st.d_scales[st.layer, mine] = scale
+    st.d_bscales.fill_(3.0)
+    k, v = st.rand(2).cuda(), st.rand(2).cuda()
+    st.handle.append_kv(st.layer, st.batch, k, v, rope=angles(60, 64).cuda())
+    theirs = [int(p) for p in st.table[1] if p >= 0]
+    rest = [p for p in range(st.P) if p not in theirs]
+    for got, was in ((st.d_cache, st.cache), (st.d_scales, st.scales)):
+        if was is None:
+            continue
+        assert torch.equal(got.cpu()[:, rest].view(torch.uint8), was[:, rest].view(torch.uint8))
+    assert (st.d_bounds[:, rest] == 77).all() and (st.d_bscales[:, rest] == 3.0).all()
+    assert (st.d_bscales[st.layer, theirs[-1]] != 3.0).all()
+
+
+def test_appended_keys_take_no_heed_of_a_free_place_s_old_table():
+    need_gpu()
+    results = []
+    for stale in (False, True):
+        st = Setup([40, 60], [0, 3], heads=2, dim=64, fp8=True, bounds=True)
+        if stale:
+            st.table[0, 2] = st.table[1, 3]
+        batch = api.Batch(st.table.cuda(), ints(st.kv_lens), 60, ints(st.starts), 3, 3)
+        st.d_scales[st.layer] = 2.0 ** -20  # grows for any new token
+        st.d_bscales.fill_(3.0)
+        k, v = st.rand(2).cuda(), st.rand(2).cuda()
+        st.handle.append_kv(st.layer, batch, k, v)
+        results.append([t.cpu().view(torch.uint8) for t in (st.d_cache, st.d_scales, st.d_bounds,
+                                                            st.d_bscales)])
     for a, b in zip(*results):
         assert torch.equal(a, b)
