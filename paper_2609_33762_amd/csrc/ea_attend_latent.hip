@@ -860,7 +860,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_latent(LatentAttendArgs a) 
   if (r - c >= rows_all) return;
   const int w0 = a.units[2 * ((int64_t)s * a.tiles_most + tile)];
   const int parts = a.units[2 * ((int64_t)s * a.tiles_most + tile) + 1];
-  if (parts <= 1) return;
+  // (with starts of rows that decrease there are more units than the host counts and
+  // launches, and nobody writes this for the last of them)
+  if (parts <= 1 || parts > a.split_grid || w0 < 0 || w0 > a.split_grid - parts) return;
   const int64_t pitch = (int64_t)(QW * 32) * (cols + 2);
   const float *first = a.parts + (int64_t)w0 * pitch;
   const float *ml = first + QW * 32 * cols + 2 * (qg * 32 + c);

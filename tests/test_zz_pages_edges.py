@@ -1,12 +1,14 @@
 """Moved, appended and attended tokens on the GPU where a block, a batch or its
 memory is out of the ordinary."""
+import ctypes as C
 import math
 
 import pytest
 import torch
 
 from gpu_common import need_gpu
-from latent_common import FP8, Latents
+from latent_common import FP8, Latents, check_attention
+from paper_2609_33762_amd import _native as N
 from paper_2609_33762_amd import api
 from test_gpu_cache_ops import Setup
 from test_zz_pages_moves import angles
@@ -176,3 +178,35 @@ def test_appended_keys_take_no_heed_of_a_free_place_s_old_table():
                                                             st.d_bscales)])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+# ------------------------------------------------------ starts that decrease
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("held", [(0x7f7f7f7f, 0x7f7f7f7f), (1 << 30, 2), (-5, 3), (809, 2)])
+def test_starts_that_decrease_stay_within_the_workspace(held, fp8):
+    # 200 of 400 sequences claim all 40 rows, 1,000 units where the host counts and
+    # launches fewer; the workspace holds numbers that are no units' places.  All
+    # sequences are one, so whoever writes a row writes the same.
+    need_gpu()
+    n, seqs, heads = 40, 400, 16
+    st = Latents([1000], [n], heads=heads, latent=512, turn=64, fp8=fp8)
+    q = st.rand(n, heads, 576)
+    d_q, guard = q.cuda(), 5
+    out = torch.full((n + guard, heads, 512), 7.0, dtype=st.act, device="cuda")
+    lse = torch.full((n + guard, heads), 7.0, device="cuda")
+    batch = api.Batch(st.table.repeat(seqs, 1).cuda(), ints([1000] * seqs), 1000,
+                      ints([0, n] * (seqs // 2) + [0]), n, n)
+    lib, ref = N.load(), C.byref
+    a = N.LatentAttention(*(N.Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (d_q, out)))
+    a.lse, a.latent_dim, a.rope_dim, a.q_heads = lse.data_ptr(), 512, 64, heads
+    a.dtype, a.scale = N.EA_BF16, 0.07
+    need = lib.ea_attend_latent_workspace(st.handle.handle, batch.ref, ref(a))
+    assert need > 1 << 20
+    ws = ints(held).repeat((need + 15) // 8 + 512)
+    assert lib.ea_attend_latent(st.handle.handle, st.layer, batch.ref, ref(a), ws.data_ptr(), need,
+                                api.current_stream()) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(ws[-1024:], ints(held).repeat(512))
+    assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()
+    check_attention(st, q, out[:n], lse[:n], 0.07, 2.0 ** -11 if fp8 else 2.0 ** -8)
