@@ -201,10 +201,11 @@ class Cache:
 
     def bound_blocks(self, d_pages, layer_begin=0, layer_count=None, dtype=None, stream=None):
         """Bounds of whole blocks from their stored keys; d_pages: int32
-        device tensor.  dtype: of a 16-bit cache (torch.bfloat16 if None)."""
+        device tensor.  dtype: of a 16-bit cache (None: kv's, torch.bfloat16
+        where kv only holds its bytes)."""
         _device_ints(d_pages, "d_pages", self._device)
         count = self.num_layers - layer_begin if layer_count is None else layer_count
-        act = N.EA_BF16 if dtype is None else _act(dtype)
+        act = self._held(dtype)
         N.check("ea_bound_blocks", self._lib.ea_bound_blocks(
             self._h, self._planes_ref, layer_begin, count, d_pages.data_ptr(), d_pages.numel(),
             act, self._stream(stream)))
@@ -257,7 +258,7 @@ class Cache:
         difference of the positions where `rope` (as for append_kv) is given.
         All arrays int32 device tensors; max_tokens and max_kv bound a
         sequence's kept tokens and the positions.  dtype: of a 16-bit cache
-        (torch.bfloat16 if None)."""
+        (None: kv's, torch.bfloat16 where kv only holds its bytes)."""
         for t, what in ((src_table, "src_table"), (dst_table, "dst_table")):
             if t.device != self._device or str(t.dtype) != "torch.int32" or t.dim() != 2 or \
                     (t.shape[1] > 1 and t.stride(1) != 1):
@@ -290,12 +291,18 @@ class Cache:
             a.rope_dim = dim
         a.interleaved, a.n_seqs, a.n_tokens = interleaved, n, tokens.numel()
         a.max_tokens, a.max_kv = max_tokens, max_kv
-        a.dtype = N.EA_BF16 if dtype is None else _act(dtype)
+        a.dtype = self._held(dtype)
         count = self.num_layers - layer_begin if layer_count is None else layer_count
         N.check("ea_move_tokens", self._lib.ea_move_tokens(
             self._h, self._planes_ref, layer_begin, count, C.byref(a), self._stream(stream)))
 
     _moved = (0, 0)  # rope_dim and latent_dim of a cache of latents
+
+    def _held(self, dtype):
+        """The type of a 16-bit cache's elements: the one given, or kv's."""
+        if dtype is not None:
+            return _act(dtype)
+        return N.EA_F16 if str(self.kv.dtype) == "torch.float16" else N.EA_BF16
 
     def _lse(self, lse, n, heads):
         if lse.device != self._device or lse.dtype not in _f32() or \

@@ -7,11 +7,11 @@ import pytest
 import torch
 
 from gpu_common import need_gpu
-from latent_common import FP8, Latents, check_attention
+from latent_common import BF16, F16, FP8, Latents, check_attention
 from paper_2609_33762_amd import _native as N
 from paper_2609_33762_amd import api
 from test_gpu_cache_ops import Setup
-from test_zz_pages_moves import angles
+from test_zz_pages_moves import Moved, angles, turn64
 
 pytestmark = pytest.mark.gpu
 
@@ -210,3 +210,42 @@ def test_starts_that_decrease_stay_within_the_workspace(held, fp8):
     assert torch.equal(ws[-1024:], ints(held).repeat(512))
     assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()
     check_attention(st, q, out[:n], lse[:n], 0.07, 2.0 ** -11 if fp8 else 2.0 ** -8)
+
+
+# ------------------------------------------------- types of 16-bit caches
+
+@pytest.mark.parametrize("act", [F16, BF16])
+def test_a_cache_s_own_type_is_the_one_its_tokens_turn_in(act):
+    # no dtype given; and one given for a cache held in bytes
+    for held in (act, torch.uint8):
+        st = Moved([100, 37], [70, 37], act=act, bounds=True)
+        if held == torch.uint8:
+            raw = st.d_cache.view(torch.uint8)
+            st.handle = api.Cache(raw, st.P, st.L, st.T, st.H, st.D, 2, bounds=st.d_bounds,
+                                  bound_scales=st.d_bscales)
+        rope = angles(st.max_kv, st.D)
+        st.move(rope=rope.cuda(), dtype=None if held == act else act)
+        st.check(rope, False, range(st.L))
+
+
+def test_latents_of_16_bit_turn_in_their_own_type():
+    st = Latents([60], [1], act=F16, latent=128, turn=32)
+    rope = angles(60, 32)
+    free = [p for p in range(st.P) if p not in st.table]
+    st.handle.move_tokens(st.table.cuda(), ints([free[:1]]), ints(range(40, 56)), ints([0, 16]),
+                          max_tokens=16, max_kv=60, rope=rope.cuda())
+    old = st.stored(0)[40:56]
+    want, mag = turn64(old[:, 128:], rope, torch.full((16,), -40), False)
+    got = st.d_cache[st.layer, free[0]].cpu().double()
+    assert torch.equal(got[:, :128], old[:, :128])
+    assert ((got[:, 128:] - want).abs() <=
+            2.0 ** -11 * want.abs() + 2.0 ** -25 + 2.0 ** -22 * mag).all()
+
+
+@pytest.mark.parametrize("act", [F16, BF16])
+def test_bounds_of_blocks_go_by_the_cache_s_own_type(act):
+    st = Moved([100], [16], act=act, bounds=True)
+    pages = [int(p) for p in st.src[0] if p >= 0][:6]
+    st.handle.bound_blocks(ints(pages))
+    for page in pages:
+        st.check_bounds(0, page, st.T, st.cache, None)
