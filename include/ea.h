@@ -766,9 +766,10 @@ typedef struct {
  * sequence s, at position p = kv_len[s] - rows + r, attends with every head to
  * the tokens j <= p of its sequence; a token's key is its whole row, its value
  * its latent.  Sums and softmax statistics are 32 bits; the weights that
- * multiply the latents are rounded to 11 bits beside f16 and fp8 latents, to 8
- * beside bf16 ones.  A row that attends to nothing gets zeros.  What lies in
- * tokens that a row does not attend to never reaches it.
+ * multiply the latents are rounded to 11 bits beside f16 and fp8 latents; beside
+ * bf16 ones to 16 bits in calls of up to 64 rows times heads a sequence (max_rows *
+ * q_heads), to 8 in larger ones.  A row that attends to nothing gets zeros.  What
+ * lies in tokens that a row does not attend to never reaches it.
  *
  * workspace: ea_attend_latent_workspace bytes (0: may be NULL), 16-byte aligned
  * device memory that a call writes before it reads: nothing in it has to be

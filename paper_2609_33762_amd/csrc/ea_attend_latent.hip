@@ -23,9 +23,13 @@
 // The reference m of a row moves only when a score is more than 2^8 above it, so
 // the sums are rarely rescaled; statistics and sums have 32 bits.  Weights are
 // rounded to 11 bits beside f16 and fp8 values (up to 2^15: 7 of shift, 8 of
-// slack), to 8 beside bf16 ones, as the products bound the kernel there: half a
-// step, 2^-8, of each, of random signs in a sum, as the result's own rounding is; a
-// second bf16 for the rest would make half of the products anew.  An fp8 value's
+// slack).  Beside bf16 ones they are the sum of two bf16, 16 bits, where sequences
+// have at most 64 columns: the two waves of four that would have none take the
+// others' columns with the second bf16, and the sums become one at the end (TWO;
+// 24 sequences of 2-4 rows of 16 heads 101 us with one bf16, 108 with two; the
+// second in the same wave, half of the products anew: 119).  With more columns they are
+// rounded to 8 bits, as the products bound the kernel there: half a step, 2^-8, of
+// each, of random signs in a sum, as the result's own rounding is.  An fp8 value's
 // scale goes into its weight before that.
 //
 // Measured (C 512, R 64, pages of 16 tokens in random order), the join included:
@@ -180,7 +184,7 @@ __device__ inline SeqTiles tiles_of(const LatentAttendArgs &a, int s) {
 // products but no bytes.
 enum Mode { kPlain, kRows, kPages };
 
-template <int ACT, bool FP8, int CT, int QW, Mode MODE>
+template <int ACT, bool FP8, int CT, int QW, Mode MODE, bool TWO>
 __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a) {
   constexpr int KG = kWaves / QW;        // groups of waves that share tokens
   constexpr int STEP = KG * 32;          // tokens of a step, 32 a group
@@ -270,7 +274,10 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   const int last_entry = over_page(kv, max(end - 1, 0));
 
   // ---- queries, the second operand of S = K Q^T: column c
-  const int my = r0 + qg * 32 + c, my_q = my / HQ;
+  // (TWO: of waves 0 and 1; the others have the same columns, and of their weights
+  // what the first bf16 leaves)
+  const int cg = TWO ? qg & 1 : qg, my = r0 + cg * 32 + c, my_q = my / HQ;
+  const bool second = TWO && qg > 1;
   const bool mine = my < rows_all;
   u32x4 qreg[KS];
   {
@@ -595,7 +602,14 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
         l += p;
         if constexpr (FP8) p *= vs[2 * j + part];
       } else {
-        ph[j >> 2][j & 3] = pack_act<PV>(y[2 * j], y[2 * j + 1]);
+        const uint32_t w = pack_act<PV>(y[2 * j], y[2 * j + 1]);
+        ph[j >> 2][j & 3] = w;
+        if constexpr (TWO) {  // the first bf16, or zeros, taken off
+          const uint32_t lo = __builtin_amdgcn_perm(w, w, second ? 0x01000c0cu : 0x0c0c0c0cu);
+          const uint32_t hi = __builtin_amdgcn_perm(w, w, second ? 0x03020c0cu : 0x0c0c0c0cu);
+          ph[j >> 2][j & 3] = pack_act<kBf16>(y[2 * j] - __uint_as_float(lo),
+                                              y[2 * j + 1] - __uint_as_float(hi));
+        }
       }
     }
   };
@@ -760,7 +774,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
                                  d) =
           u32x2{pack_act<ACT>(v[0] * norm, v[1] * norm), pack_act<ACT>(v[2] * norm, v[3] * norm)};
     else
-      *reinterpret_cast<f32x4 *>(part_of + qg * 32 * cols +
+      *reinterpret_cast<f32x4 *>(part_of + cg * 32 * cols +
                                  ((dt * 4 + i4) * kLanes + lane) * 4) = v;
   };
   auto emit_statistics = [&](float ref, float total) {
@@ -777,15 +791,49 @@ __global__ __launch_bounds__(kThreads, 1) void attend_latent(LatentAttendArgs a)
   }
   if constexpr (KG == 1) {
     const float norm = total_of == 0.f ? 0.f : 1.f / total_of;
+    auto tile_of_o = [&](int dt, int i4) {
+      return f32x4{o[dt][i4 * 4], o[dt][i4 * 4 + 1], o[dt][i4 * 4 + 2], o[dt][i4 * 4 + 3]};
+    };
+    if constexpr (TWO) {  // both waves of a column have half of its tiles' sums to join
+      constexpr int HALF = DT / 2;
+      static_assert(kWaves * HALF * 4 * kLanes * 16 <= BYTES, "every wave's other half");
+      f32x4 *sums = reinterpret_cast<f32x4 *>(ring) + lane;
+      auto give = [&](int first) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
+        for (int dt = 0; dt < HALF; ++dt) {
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
-        emit(dt, i4,
-             f32x4{o[dt][i4 * 4], o[dt][i4 * 4 + 1], o[dt][i4 * 4 + 2],
-                   o[dt][i4 * 4 + 3]},
-             norm);
-      __builtin_amdgcn_sched_barrier(0);
+          for (int i4 = 0; i4 < 4; ++i4)
+            sums[((wave * HALF + dt) * 4 + i4) * kLanes] = tile_of_o(first + dt, i4);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      auto take = [&](int first) {
+#pragma unroll
+        for (int dt = 0; dt < HALF; ++dt) {
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4)
+            emit(first + dt, i4,
+                 tile_of_o(first + dt, i4) + sums[(((wave ^ 2) * HALF + dt) * 4 + i4) * kLanes],
+                 norm);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      __syncthreads();  // the ring has been read
+      if (second) give(0);
+      else give(HALF);
+      __syncthreads();
+      if (second) {
+        take(HALF);
+        return;
+      }
+      take(0);
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) emit(dt, i4, tile_of_o(dt, i4), norm);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     emit_statistics(ref_of, total_of);
   } else {
@@ -942,10 +990,14 @@ void go(void (*kernel)(LatentAttendArgs), const LatentAttendArgs &a, hipStream_t
 template <int ACT, bool FP8, int CT, Mode MODE>
 hipError_t columns(const LatentAttendArgs &a, hipStream_t s) {
   if constexpr (FP8) {
-    if (a.wave_columns == 1) go(attend_latent<ACT, true, CT, 1, MODE>, a, s);
-    if (a.wave_columns == 2) go(attend_latent<ACT, true, CT, 2, MODE>, a, s);
+    if (a.wave_columns == 1) go(attend_latent<ACT, true, CT, 1, MODE, false>, a, s);
+    if (a.wave_columns == 2) go(attend_latent<ACT, true, CT, 2, MODE, false>, a, s);
   }
-  if (a.wave_columns == 4) go(attend_latent<ACT, FP8, CT, 4, MODE>, a, s);
+  constexpr bool BF16 = ACT == kBf16 && !FP8;
+  if constexpr (BF16)
+    if (a.two_weights) go(attend_latent<ACT, false, CT, 4, MODE, true>, a, s);
+  if (a.wave_columns == 4 && !(BF16 && a.two_weights))
+    go(attend_latent<ACT, FP8, CT, 4, MODE, false>, a, s);
   if (a.slices > 0)
     hipLaunchKernelGGL(join_latent<ACT>,
                        dim3((unsigned)a.b.n_seqs * a.tiles_most * a.wave_columns * a.slices),

@@ -113,6 +113,7 @@ struct LatentAttendArgs {
   int32_t *units;           // [n_seqs][tiles_most][2]: a unit's first workgroup, its parts
   float *parts;             // [split_grid][32 * wave_columns][latent, whole 32, + 2]
   int32_t slices;           // workgroups that join a unit's 32 rows; 0: nothing is split
+  int32_t two_weights;      // beside bf16 latents: weights are the sum of two bf16
 };
 
 struct LatentAppendArgs {

@@ -153,6 +153,11 @@ int ea_attend_latent(ea_cache *c, int32_t layer, const ea_batch *b, const ea_lat
   k.units = static_cast<int32_t *>(workspace);
   k.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.unit_bytes);
   k.slices = p.slices;
+  // Half of the waves have no columns then, and bf16 latents get weights of 16 bits for
+  // 0 to 10% of the time (64 sequences of 8,192-65,536 tokens, 16 heads: 689 us with 8
+  // bits, 736 with 16; 64 heads: 729, 801; 300 of 500-16,000: 826, 847; one of
+  // 65,536: 47.6, 47.8).
+  k.two_weights = (int64_t)b->max_rows * a->q_heads <= 64;
   OnDevice on(ea::cache_device(c));
   KV_HIP(on.status());
   KV_HIP(ea::launch_attend_latent(k, a->dtype, ea::cache_desc(c).elem_bytes == 1, stream));
