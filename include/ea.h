@@ -629,8 +629,8 @@ typedef struct {
  * then the older codes are requantised to it.  Values that are not finite
  * become NaN.  With bounds, the touched blocks' bounds are made from all
  * their stored keys.  Pages that get new tokens must belong to one sequence
- * of the batch alone; a prefix shared by several is fine.  Of a sequence without
- * rows in the step (a free place of a padded batch) nothing is read or written,
+ * of the batch alone; a prefix shared by several is fine.  No page of a sequence
+ * without rows in the step (a free place of a padded batch) is read or written,
  * whatever its length and table say. */
 int ea_append_kv(ea_cache *cache, const ea_cache_planes *planes, int32_t layer,
                  const ea_batch *batch, const ea_append *args, hipStream_t stream);

@@ -36,7 +36,7 @@
 // 64 sequences of 8,192-65,536 tokens, a row of 16 heads, fp8: 305 us (4.6 TB/s; its
 // loads alone 266); 2,048 rows of 16 heads over 26,624 tokens, bf16: 1.60-1.68 ms
 // (1.09-1.14 PFLOP/s; without its loads 1.29 ms); 65,536 tokens, a row of 128 heads,
-// bf16: 62 us, 42-46 of them before the join; 24 sequences of 2-4 rows, bf16: 90 us.
+// bf16: 65 us, 42-46 of them before the join; 24 sequences of 2-4 rows, bf16: 97 us.
 #include <hip/hip_runtime.h>
 
 #include "ea_kv_device.hpp"
